@@ -209,6 +209,101 @@ moda_status moda_attn_decode_noalloc(const void* Q, const void* Kseq, const void
                                      const moda_shape* s, void* hip_stream);
 
 /*
+ * A shared and a bounded sequence cache.  The calls below serve batches whose sequences differ in length,
+ * share what they begin with, and drop the rows that attention no longer looks at.
+ *
+ * Lengths: `lengths` (device, int32, [B], 4-byte aligned) holds the filled rows of each sequence's cache; NULL:
+ * all have s->T.  s->T bounds them: a value below 0 counts as 0, one above s->T as s->T.  Rows from a
+ * sequence's length on are never read for their values, and what belongs to them is left as it was.
+ *
+ * Accumulated weights: an fp32 array [B, Hk, kv_alloc] beside the cache.  A call that adds to it takes
+ * weights_in (NULL: zeros) and weights_out; the two may be the same array, and may not overlap otherwise.
+ */
+
+/* Prefixes that groups of sequences share: sequence b reads prefix b / (B / n_prefixes). */
+typedef struct {
+  int32_t n_prefixes;   /* > 0, B % n_prefixes == 0                                      */
+  int32_t prefix_rows;  /* rows attended of every prefix, >= 0                           */
+  int32_t prefix_alloc; /* rows allocated of every prefix, >= prefix_rows                */
+} moda_prefix;
+
+/*
+ * Decoding step of a batch whose sequences share prefixes: for each of the B new tokens ONE softmax over the
+ * rows of its prefix, the rows of its own cache and its depth slots.  The rows of a prefix are read once for all the
+ * sequences that share it, not once for each.
+ *   in : Q                 [B, Hq, d]
+ *        Kprefix, Vprefix  [n_prefixes, Hk, prefix_alloc, d]  (NULL iff prefix_rows == 0; `prefix` NULL: no prefix)
+ *        Kseq, Vseq        [B, Hk, kv_alloc, d]               (NULL allowed iff s->T == 0)
+ *        Kdepth, Vdepth    [B, Hk, depth_alloc, d]            (NULL allowed iff depth_count == 0)
+ *        prefix_lengths    [n_prefixes] or NULL (all prefix_rows), read as `lengths` is
+ *        lengths           [B] or NULL
+ *        weights_in        [B, Hk, kv_alloc] fp32 or NULL
+ *   out: O [B, Hq, d], LSE [B, Hq] fp32; weights_out or NULL: weights_out[b,g,j] = weights_in[b,g,j] + the sum over
+ *        the query heads h of group g of exp(logit of row j - LSE[b,h]), for the rows j of the own cache
+ *   workspace: at least moda_attn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned; contents on entry
+ *        are ignored.  `with_weights`: whether weights_out will be given.
+ * A token that sees nothing (all lengths 0, no slots), or whose logits are all -inf, gets O = 0, LSE = -inf and
+ * adds no weight.  s->causal is ignored.  bf16 only.  kv_alloc >= s->T >= 0.
+ */
+size_t moda_attn_decode_shared_workspace_bytes(const moda_prefix* prefix, int with_weights, const moda_shape* s);
+moda_status moda_attn_decode_shared(const void* Q, const void* Kprefix, const void* Vprefix, const void* Kseq,
+                                    const void* Vseq, const void* Kdepth, const void* Vdepth,
+                                    const int32_t* prefix_lengths, const int32_t* lengths, const float* weights_in,
+                                    float* weights_out, void* O, float* LSE, int32_t kv_alloc, void* workspace,
+                                    size_t workspace_bytes, const moda_prefix* prefix, const moda_shape* s,
+                                    void* hip_stream);
+
+/*
+ * The decoding step that keeps account of what it looks at: moda_attn_decode_shared without a prefix and with
+ * weights_out (required).  Workspace: moda_attn_decode_shared_workspace_bytes(NULL, 1, s).
+ */
+moda_status moda_attn_decode_weights(const void* Q, const void* Kseq, const void* Vseq, const void* Kdepth,
+                                     const void* Vdepth, const int32_t* lengths, const float* weights_in,
+                                     float* weights_out, void* O, float* LSE, int32_t kv_alloc, void* workspace,
+                                     size_t workspace_bytes, const moda_shape* s, void* hip_stream);
+
+/*
+ * The attention weight that every key of a prompt has gathered, from the forward pass in hand:
+ *   weights_out[b,g,j] = weights_in[b,g,j] + sum over the query heads h of group g and the queries t that see row j
+ *                        (t >= j where causal) of exp(scale * <Q[b,h,t], Kseq[b,g,j]> - LSE[b,h,t])
+ * for j < length of b, over the queries t < length of b; window > 0: over the last `window` of them only (0: all).
+ * With depth slots the LSE of the forward pass covers them too, and the weights are those of that softmax.
+ *   in : Q [B, Hq, T, d]; Kseq [B, Hk, kv_alloc, d], kv_alloc >= T; LSE [B, Hq, T] fp32; lengths [B] or NULL;
+ *        weights_in [B, Hk, kv_alloc] fp32 or NULL
+ *   out: weights_out [B, Hk, kv_alloc] fp32
+ *   workspace: at least moda_attn_weights_workspace_bytes(...) bytes (may be 0: then NULL is accepted), 16-byte aligned
+ * bf16 and fp32.  depth_alloc and depth_count of `s` are not used.
+ */
+size_t moda_attn_weights_workspace_bytes(int32_t window, const moda_shape* s);
+moda_status moda_attn_weights(const void* Q, const void* Kseq, const float* LSE, const int32_t* lengths,
+                              const float* weights_in, float* weights_out, int32_t window, int32_t kv_alloc,
+                              void* workspace, size_t workspace_bytes, const moda_shape* s, void* hip_stream);
+
+/*
+ * Eviction: each (sequence, key/value head) keeps min(keep, length) of its rows, chosen in this order:
+ * first the rows whose position is above the largest position among its filled rows less `recent` (whatever they weigh),
+ * then by weight from the heaviest on (a NaN counts as lighter than everything else); ties go to the lowest row.  positions [B, Hk, kv_alloc] int32
+ * holds the token position of every row; NULL: a row's position is its row number (a cache that nothing has left yet).
+ * The kept rows take the rows [0, min(keep, length)): one that lies there already stays where it is, the others fill the
+ * places of the evicted rows, both in ascending order.  Softmax attention does not depend on the order of the rows.
+ *   in : Kseq, Vseq [B, Hk, kv_alloc, d]; weights [B, Hk, kv_alloc] fp32; positions or NULL; lengths [B] or NULL
+ *   out: Kout, Vout [B, Hk, out_alloc, d], weights_out [B, Hk, out_alloc], positions_out (iff positions) the same:
+ *        the kept rows, out_alloc >= min(keep, T); rows behind them are left as they were
+ *        lengths_out [B] or NULL: min(keep, length); may be `lengths` itself
+ *        index [B, Hk, min(keep, T)] int32: the row that each row came from, -1 from the new length on
+ * In place: Kout == Kseq, Vout == Vseq, weights_out == weights, positions_out == positions and out_alloc == kv_alloc;
+ * only the rows that change their place are then moved.  Otherwise outputs must not overlap inputs.
+ *   workspace: at least moda_cache_evict_workspace_bytes(...) bytes, 16-byte aligned
+ * s->T >= 1, keep >= 1, 0 <= recent <= keep.  bf16 and fp32.  Hq, depth_alloc, depth_count, causal and scale of `s` are not used.
+ */
+size_t moda_cache_evict_workspace_bytes(int32_t keep, const moda_shape* s);
+moda_status moda_cache_evict(const void* Kseq, const void* Vseq, const float* weights, const int32_t* positions,
+                             const int32_t* lengths, void* Kout, void* Vout, float* weights_out,
+                             int32_t* positions_out, int32_t* lengths_out, int32_t* index, int32_t keep,
+                             int32_t recent, int32_t kv_alloc, int32_t out_alloc, void* workspace,
+                             size_t workspace_bytes, const moda_shape* s, void* hip_stream);
+
+/*
  * Measurement aid: a kernel whose loop holds nothing but the bf16 matrix instruction the
  * attention kernels use (v_mfma_f32_32x32x16_bf16; eight waves per workgroup, four independent
  * accumulators per wave), for reporting what the matrix pipe of THIS chip sustains next to its

@@ -24,6 +24,9 @@ MODA_F32, MODA_BF16 = 0, 1
 EXPORTS = ("moda_attn_fwd", "moda_attn_fwd_tuned", "moda_attn_bwd_workspace_bytes", "moda_attn_bwd", "moda_depth_append",
            "moda_attn_decode", "moda_attn_decode_workspace_bytes", "moda_attn_decode_noalloc",
            "moda_attn_decode_noalloc_max_bytes",
+           "moda_attn_decode_shared", "moda_attn_decode_shared_workspace_bytes", "moda_attn_decode_weights",
+           "moda_attn_weights", "moda_attn_weights_workspace_bytes",
+           "moda_cache_evict", "moda_cache_evict_workspace_bytes",
            "moda_calibrate_mfma", "moda_calibrate_mfma_operand_bytes", "moda_calibrate_mfma_sink_bytes",
            "moda_status_string", "moda_version", "moda_kernels_per_call", "moda_fwd_kernel_name",
            "moda_bwd_kernel_name")
@@ -39,6 +42,10 @@ class MODAShape(ctypes.Structure):
 class MODAFwdTuning(ctypes.Structure):
     _fields_ = [("waves", ctypes.c_int32), ("heads_per_tile", ctypes.c_int32), ("head_group", ctypes.c_int32),
                 ("depth_path", ctypes.c_int32)]
+
+
+class MODAPrefix(ctypes.Structure):
+    _fields_ = [("n_prefixes", ctypes.c_int32), ("prefix_rows", ctypes.c_int32), ("prefix_alloc", ctypes.c_int32)]
 
 
 class MODAError(RuntimeError):
@@ -78,6 +85,21 @@ def lib():
         L.moda_attn_decode_noalloc.restype = ctypes.c_int
         L.moda_attn_decode_noalloc_max_bytes.argtypes = []
         L.moda_attn_decode_noalloc_max_bytes.restype = ctypes.c_size_t
+        i32, size, xp = ctypes.c_int32, ctypes.c_size_t, ctypes.POINTER(MODAPrefix)
+        L.moda_attn_decode_shared_workspace_bytes.argtypes = [xp, ctypes.c_int, sp]
+        L.moda_attn_decode_shared_workspace_bytes.restype = size
+        L.moda_attn_decode_shared.argtypes = [vp] * 13 + [i32, vp, size, xp, sp, vp]
+        L.moda_attn_decode_shared.restype = ctypes.c_int
+        L.moda_attn_decode_weights.argtypes = [vp] * 10 + [i32, vp, size, sp, vp]
+        L.moda_attn_decode_weights.restype = ctypes.c_int
+        L.moda_attn_weights_workspace_bytes.argtypes = [i32, sp]
+        L.moda_attn_weights_workspace_bytes.restype = size
+        L.moda_attn_weights.argtypes = [vp] * 6 + [i32, i32, vp, size, sp, vp]
+        L.moda_attn_weights.restype = ctypes.c_int
+        L.moda_cache_evict_workspace_bytes.argtypes = [i32, sp]
+        L.moda_cache_evict_workspace_bytes.restype = size
+        L.moda_cache_evict.argtypes = [vp] * 11 + [i32] * 4 + [vp, size, sp, vp]
+        L.moda_cache_evict.restype = ctypes.c_int
         L.moda_calibrate_mfma_operand_bytes.argtypes = []
         L.moda_calibrate_mfma_operand_bytes.restype = ctypes.c_size_t
         L.moda_calibrate_mfma_sink_bytes.argtypes = [ctypes.c_int32]
@@ -316,6 +338,153 @@ def moda_attn_decode(Q, Kseq, Vseq, Kdepth=None, Vdepth=None, T=None, depth_coun
                                       _ptr(lse), int(kv_alloc), _ptr(workspace), ws_bytes, ctypes.byref(s),
                                       _stream(dev)))
     return out, lse
+
+
+def _workspace(workspace, need, device):
+    if workspace is None:
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous tensor on Q's device")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _decode_shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T, depth_count, scale,
+                   weights, weights_out, out, lse, workspace):
+    B, Hq, d = Q.shape
+    if Kseq is None and Kprefix is None:
+        raise ValueError("Kseq or Kprefix must be given")
+    Hk = (Kprefix if Kseq is None else Kseq).shape[1]
+    kv_alloc = 0 if Kseq is None else Kseq.shape[2]
+    T = kv_alloc if T is None else int(T)
+    La = 0 if Kdepth is None else Kdepth.shape[2]
+    L = La if depth_count is None else int(depth_count)
+    Np, prefix_alloc = (1, 0) if Kprefix is None else (Kprefix.shape[0], Kprefix.shape[2])
+    P = prefix_alloc if P is None else int(P)
+    dev, dt = Q.device, Q.dtype
+    _require(Q, "Q", (B, Hq, d), dt, dev)
+    _require(Kprefix, "Kprefix", (Np, Hk, prefix_alloc, d), dt, dev)
+    _require(Vprefix, "Vprefix", (Np, Hk, prefix_alloc, d), dt, dev)
+    _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
+    _require(Vseq, "Vseq", (B, Hk, kv_alloc, d), dt, dev)
+    _require(Kdepth, "Kdepth", (B, Hk, La, d), dt, dev)
+    _require(Vdepth, "Vdepth", (B, Hk, La, d), dt, dev)
+    _require(prefix_lengths, "prefix_lengths", (Np,), torch.int32, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
+    _require(weights_out, "weights_out", (B, Hk, kv_alloc), torch.float32, dev)
+    s = MODAShape(B, Hq, Hk, T, d, La, L, 1, float(scale) if scale else 0.0, _dtype_code(Q))
+    x = MODAPrefix(Np, P, prefix_alloc)
+    if out is None:
+        out = torch.empty_like(Q)
+    if lse is None:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+    _require(out, "out", Q.shape, dt, dev)
+    _require(lse, "lse", (B, Hq), torch.float32, dev)
+    need = 0
+    if workspace is None:
+        need = int(lib().moda_attn_decode_shared_workspace_bytes(ctypes.byref(x), int(weights_out is not None), ctypes.byref(s)))
+    workspace, ws_bytes = _workspace(workspace, need, dev)
+    with torch.cuda.device(dev):
+        _check(lib().moda_attn_decode_shared(
+            _ptr(Q), _ptr(Kprefix), _ptr(Vprefix), _ptr(Kseq), _ptr(Vseq), _ptr(Kdepth), _ptr(Vdepth),
+            _ptr(prefix_lengths), _ptr(lengths), _ptr(weights), _ptr(weights_out), _ptr(out), _ptr(lse), kv_alloc,
+            _ptr(workspace), ws_bytes, ctypes.byref(x), ctypes.byref(s), _stream(dev)))
+    return out, lse
+
+
+def moda_attn_decode_shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth=None, Vdepth=None, prefix_lengths=None, lengths=None,
+                            P=None, T=None, depth_count=None, scale=None, weights=None, weights_out=None, out=None,
+                            lse=None, workspace=None):
+    """O [B,Hq,d], LSE [B,Hq] for one new token per sequence, under one softmax over the rows of its prefix, of its own
+    cache and its depth slots.  Kprefix/Vprefix [n_prefixes,Hk,prefix_alloc,d]: sequence b reads prefix
+    b // (B / n_prefixes), whose rows are read once for all that share it.  Kseq/Vseq [B,Hk,kv_alloc,d] (None: no own
+    rows), Kdepth/Vdepth [B,Hk,depth_alloc,d] or None.  P and T bound the rows attended (default: all allocated), the int32
+    tensors prefix_lengths [n_prefixes] and lengths [B] give them for each.  With weights [B,Hk,kv_alloc] (fp32) the own
+    rows' attention weights, summed over the heads of a group, are added to it, in place or, with weights_out, into that."""
+    if weights_out is None:
+        weights_out = weights
+    return _decode_shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T, depth_count,
+                          scale, weights, weights_out, out, lse, workspace)
+
+
+def moda_attn_decode_weights(Q, Kseq, Vseq, weights=None, Kdepth=None, Vdepth=None, lengths=None, T=None, depth_count=None,
+                             scale=None, weights_out=None, out=None, lse=None, workspace=None):
+    """O [B,Hq,d], LSE [B,Hq], weights for one new token per sequence: the decoding step over caches of `lengths` [B] rows
+    each (default: T), which adds the attention weight of every row, summed over the heads of a group, to
+    weights [B,Hk,kv_alloc] (fp32): in place, or into weights_out.  weights None: they start from zero."""
+    if weights_out is None:
+        weights_out = weights if weights is not None else torch.zeros(Kseq.shape[:3], dtype=torch.float32, device=Q.device)
+    out, lse = _decode_shared(Q, None, None, Kseq, Vseq, Kdepth, Vdepth, None, lengths, None, T, depth_count, scale,
+                              weights, weights_out, out, lse, workspace)
+    return out, lse, weights_out
+
+
+def moda_attn_weights(Q, Kseq, LSE, window=0, causal=True, scale=None, lengths=None, weights=None, weights_out=None,
+                      workspace=None):
+    """weights [B,Hk,kv_alloc] (fp32): the attention weight that each row of Kseq [B,Hk,kv_alloc,d] gets from the queries
+    Q [B,Hq,T,d] (T <= kv_alloc) whose log-sum-exp LSE [B,Hq,T] the forward pass left, summed over queries and the heads of
+    a group; of the last `window` queries only unless that is 0.  lengths [B] (int32): the filled positions of each
+    sequence.  Added to `weights` where given, in place unless weights_out is."""
+    B, Hq, T, d = Q.shape
+    Hk, kv_alloc = Kseq.shape[1], Kseq.shape[2]
+    dev, dt = Q.device, Q.dtype
+    _require(Q, "Q", (B, Hq, T, d), dt, dev)
+    _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
+    _require(LSE, "LSE", (B, Hq, T), torch.float32, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    if weights_out is None:
+        weights_out = weights if weights is not None else torch.zeros((B, Hk, kv_alloc), dtype=torch.float32, device=dev)
+    _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
+    _require(weights_out, "weights_out", (B, Hk, kv_alloc), torch.float32, dev)
+    s = MODAShape(B, Hq, Hk, T, d, 0, 0, int(bool(causal)), float(scale) if scale else 0.0, _dtype_code(Q))
+    need = int(lib().moda_attn_weights_workspace_bytes(int(window), ctypes.byref(s))) if workspace is None else 0
+    workspace, ws_bytes = _workspace(workspace, need, dev)
+    with torch.cuda.device(dev):
+        _check(lib().moda_attn_weights(_ptr(Q), _ptr(Kseq), _ptr(LSE), _ptr(lengths), _ptr(weights), _ptr(weights_out),
+                                       int(window), kv_alloc, _ptr(workspace), ws_bytes, ctypes.byref(s), _stream(dev)))
+    return weights_out
+
+
+def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, lengths=None, T=None, out=None, lengths_out=None,
+                     index=None, workspace=None):
+    """index [B,Hk,min(keep,T)], lengths [B] (both int32): each (sequence, key/value head) keeps its `recent` newest rows and
+    the heaviest others, `keep` in all.  Kseq/Vseq [B,Hk,kv_alloc,d], weights [B,Hk,kv_alloc] (fp32), positions
+    [B,Hk,kv_alloc] (int32, the rows' token positions; None: their row numbers), of which lengths [B] (None: T, None: all)
+    rows are filled.  The kept rows end up in rows [0, new length): in place, or, with out = (Kout, Vout, weights_out,
+    positions_out or None) of out_alloc >= min(keep, T) rows, there.  index: the row that each came from, -1 behind them.
+    Without lengths_out a call in place overwrites `lengths`, if given; else the new lengths are a new tensor."""
+    B, Hk, kv_alloc, d = Kseq.shape
+    T = kv_alloc if T is None else int(T)
+    keep, n = int(keep), max(0, min(int(keep), T))
+    dev, dt = Kseq.device, Kseq.dtype
+    Kout, Vout, W_out, P_out = (Kseq, Vseq, weights, positions) if out is None else out
+    if Kout.dim() != 4:
+        raise ValueError("Kout: expected a [B,Hk,out_alloc,d] tensor")
+    out_alloc = Kout.shape[2]
+    _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
+    _require(Vseq, "Vseq", (B, Hk, kv_alloc, d), dt, dev)
+    _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
+    _require(positions, "positions", (B, Hk, kv_alloc), torch.int32, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    _require(Kout, "Kout", (B, Hk, out_alloc, d), dt, dev)
+    _require(Vout, "Vout", (B, Hk, out_alloc, d), dt, dev)
+    _require(W_out, "weights_out", (B, Hk, out_alloc), torch.float32, dev)
+    _require(P_out, "positions_out", (B, Hk, out_alloc), torch.int32, dev)
+    if lengths_out is None:
+        lengths_out = lengths if lengths is not None and out is None else torch.empty(B, dtype=torch.int32, device=dev)
+    if index is None:
+        index = torch.empty((B, Hk, n), dtype=torch.int32, device=dev)
+    _require(lengths_out, "lengths_out", (B,), torch.int32, dev)
+    _require(index, "index", (B, Hk, n), torch.int32, dev)
+    s = MODAShape(B, Hk, Hk, T, d, 0, 0, 1, 0.0, _dtype_code(Kseq))
+    need = int(lib().moda_cache_evict_workspace_bytes(keep, ctypes.byref(s))) if workspace is None else 0
+    workspace, ws_bytes = _workspace(workspace, need, dev)
+    with torch.cuda.device(dev):
+        _check(lib().moda_cache_evict(
+            _ptr(Kseq), _ptr(Vseq), _ptr(weights), _ptr(positions), _ptr(lengths), _ptr(Kout), _ptr(Vout), _ptr(W_out),
+            _ptr(P_out), _ptr(lengths_out), _ptr(index), keep, int(recent), kv_alloc, out_alloc, _ptr(workspace), ws_bytes,
+            ctypes.byref(s), _stream(dev)))
+    return index, lengths_out
 
 
 def moda_calibrate_mfma(operands, workgroups, iters, sink=None):

@@ -364,6 +364,154 @@ static moda_status decode_with(const void* Q, const void* Kseq, const void* Vseq
                                                 static_cast<hipStream_t>(hip_stream)));
 }
 
+// ---------------------------------------------------------------- a shared and a bounded sequence cache
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static const moda_prefix kNoPrefix = {1, 0, 0};
+
+static moda_status check_shared(const moda_prefix* x, const moda_shape* s) {
+  const moda_status st = check_dims(s);
+  if (st != MODA_OK) return st;
+  if (s->dtype != MODA_BF16) return MODA_ERR_UNSUPPORTED;
+  if (x->n_prefixes <= 0 || x->prefix_rows < 0 || x->prefix_alloc < x->prefix_rows) return MODA_ERR_SHAPE;
+  if (s->B % x->n_prefixes != 0) return MODA_ERR_SHAPE;
+  return MODA_OK;
+}
+
+static moda::SharedParams shared_dims(const moda_prefix* x, const moda_shape* s) {
+  moda::SharedParams p{};
+  p.B = s->B; p.Hq = s->Hq; p.Hk = s->Hk; p.T = s->T;
+  p.Np = x->n_prefixes; p.P = x->prefix_rows; p.P_alloc = x->prefix_alloc;
+  p.depth_alloc = s->depth_alloc; p.depth_count = s->depth_count;
+  return p;
+}
+
+size_t moda_attn_decode_shared_workspace_bytes(const moda_prefix* prefix, int with_weights, const moda_shape* s) {
+  const moda_prefix* x = prefix ? prefix : &kNoPrefix;
+  if (check_shared(x, s) != MODA_OK || s->B == 0) return 0;
+  return moda::decode_shared_workspace_bytes(shared_dims(x, s), s->d, with_weights != 0);
+}
+
+moda_status moda_attn_decode_shared(const void* Q, const void* Kprefix, const void* Vprefix, const void* Kseq,
+                                    const void* Vseq, const void* Kdepth, const void* Vdepth,
+                                    const int32_t* prefix_lengths, const int32_t* lengths, const float* weights_in,
+                                    float* weights_out, void* O, float* LSE, int32_t kv_alloc, void* workspace,
+                                    size_t workspace_bytes, const moda_prefix* prefix, const moda_shape* s,
+                                    void* hip_stream) {
+  const moda_prefix* x = prefix ? prefix : &kNoPrefix;
+  moda_status st = check_shared(x, s);
+  if (st != MODA_OK) return st;
+  if (kv_alloc < s->T) return MODA_ERR_SHAPE;
+  if (s->B == 0) return MODA_OK;
+  if (!Q || !O || !LSE) return MODA_ERR_NULL;
+  if (x->prefix_rows > 0 && (!Kprefix || !Vprefix)) return MODA_ERR_NULL;
+  if (s->T > 0 && (!Kseq || !Vseq)) return MODA_ERR_NULL;
+  if (s->depth_count > 0 && (!Kdepth || !Vdepth)) return MODA_ERR_NULL;
+  if (weights_in && !weights_out) return MODA_ERR_NULL;
+  const void* ptrs[] = {Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, weights_in, weights_out, O, LSE, workspace};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return MODA_ERR_ALIGN;
+  if (!aligned4(prefix_lengths) || !aligned4(lengths)) return MODA_ERR_ALIGN;
+
+  moda::SharedParams p = shared_dims(x, s);
+  p.T_alloc = kv_alloc;
+  if (!workspace || workspace_bytes < moda::decode_shared_workspace_bytes(p, s->d, weights_out != nullptr))
+    return MODA_ERR_WORKSPACE;
+  p.Q = Q; p.Kp = Kprefix; p.Vp = Vprefix; p.Ks = Kseq; p.Vs = Vseq; p.Kd = Kdepth; p.Vd = Vdepth;
+  p.prefix_lengths = prefix_lengths; p.lengths = lengths;
+  p.w_in = weights_in; p.w_out = weights_out;
+  p.O = O; p.LSE = LSE;
+  p.scale = resolve_scale(s);
+  p.scale_log2 = p.scale * 1.4426950408889634f;
+  return launch_status(moda::launch_decode_shared(p, s->d, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+moda_status moda_attn_decode_weights(const void* Q, const void* Kseq, const void* Vseq, const void* Kdepth,
+                                     const void* Vdepth, const int32_t* lengths, const float* weights_in,
+                                     float* weights_out, void* O, float* LSE, int32_t kv_alloc, void* workspace,
+                                     size_t workspace_bytes, const moda_shape* s, void* hip_stream) {
+  const moda_status st = check_shared(&kNoPrefix, s);
+  if (st != MODA_OK) return st;
+  if (kv_alloc < s->T) return MODA_ERR_SHAPE;
+  if (s->B == 0) return MODA_OK;
+  if (s->T > 0 && !weights_out) return MODA_ERR_NULL;
+  return moda_attn_decode_shared(Q, nullptr, nullptr, Kseq, Vseq, Kdepth, Vdepth, nullptr, lengths, weights_in,
+                                 weights_out, O, LSE, kv_alloc, workspace, workspace_bytes, nullptr, s, hip_stream);
+}
+
+static moda::WeightsParams weights_dims(int32_t window, const moda_shape* s) {
+  moda::WeightsParams p{};
+  p.B = s->B; p.Hq = s->Hq; p.Hk = s->Hk; p.T = s->T;
+  p.window = window > 0 ? window : s->T;
+  p.causal = s->causal;
+  return p;
+}
+
+size_t moda_attn_weights_workspace_bytes(int32_t window, const moda_shape* s) {
+  if (check_shape(s) != MODA_OK || window < 0 || s->B == 0 || s->T == 0) return 0;
+  return moda::weights_workspace_bytes(weights_dims(window, s), s->d, s->dtype == MODA_F32);
+}
+
+moda_status moda_attn_weights(const void* Q, const void* Kseq, const float* LSE, const int32_t* lengths,
+                              const float* weights_in, float* weights_out, int32_t window, int32_t kv_alloc,
+                              void* workspace, size_t workspace_bytes, const moda_shape* s, void* hip_stream) {
+  const moda_status st = check_shape(s);
+  if (st != MODA_OK) return st;
+  if (window < 0 || kv_alloc < s->T) return MODA_ERR_SHAPE;
+  if (s->B == 0 || s->T == 0) return MODA_OK;
+  if (!Q || !Kseq || !LSE || !weights_out) return MODA_ERR_NULL;
+  const void* ptrs[] = {Q, Kseq, LSE, weights_in, weights_out, workspace};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return MODA_ERR_ALIGN;
+  if (!aligned4(lengths)) return MODA_ERR_ALIGN;
+  moda::WeightsParams p = weights_dims(window, s);
+  const bool f32 = s->dtype == MODA_F32;
+  const size_t need = moda::weights_workspace_bytes(p, s->d, f32);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return MODA_ERR_WORKSPACE;
+  p.Q = Q; p.K = Kseq; p.LSE = LSE; p.lengths = lengths; p.w_in = weights_in; p.w_out = weights_out;
+  p.T_alloc = kv_alloc;
+  p.scale_log2 = resolve_scale(s) * 1.4426950408889634f;
+  return launch_status(moda::launch_weights(p, s->d, f32, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t moda_cache_evict_workspace_bytes(int32_t keep, const moda_shape* s) {
+  if (check_dims(s) != MODA_OK || keep < 1 || s->B == 0 || s->T < 1) return 0;
+  return moda::evict_workspace_bytes(s->B, s->Hk, s->T, keep);
+}
+
+moda_status moda_cache_evict(const void* Kseq, const void* Vseq, const float* weights, const int32_t* positions,
+                             const int32_t* lengths, void* Kout, void* Vout, float* weights_out,
+                             int32_t* positions_out, int32_t* lengths_out, int32_t* index, int32_t keep,
+                             int32_t recent, int32_t kv_alloc, int32_t out_alloc, void* workspace,
+                             size_t workspace_bytes, const moda_shape* s, void* hip_stream) {
+  const moda_status st = check_dims(s);
+  if (st != MODA_OK) return st;
+  if (s->T < 1 || keep < 1 || recent < 0 || recent > keep || kv_alloc < s->T) return MODA_ERR_SHAPE;
+  const int n = std::min(keep, s->T);
+  if (out_alloc < n) return MODA_ERR_SHAPE;
+  if (s->B == 0) return MODA_OK;
+  if (!Kseq || !Vseq || !weights || !Kout || !Vout || !weights_out || !index) return MODA_ERR_NULL;
+  if ((positions == nullptr) != (positions_out == nullptr)) return MODA_ERR_NULL;
+  const bool in_place = Kout == Kseq;
+  if ((Vout == Vseq) != in_place || (weights_out == weights) != in_place) return MODA_ERR_SHAPE;
+  if (positions && (positions_out == positions) != in_place) return MODA_ERR_SHAPE;
+  if (in_place && out_alloc != kv_alloc) return MODA_ERR_SHAPE;
+  const void* ptrs[] = {Kseq, Vseq, weights, positions, Kout, Vout, weights_out, positions_out, index, workspace};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return MODA_ERR_ALIGN;
+  if (!aligned4(lengths) || !aligned4(lengths_out)) return MODA_ERR_ALIGN;
+  if (!workspace || workspace_bytes < moda::evict_workspace_bytes(s->B, s->Hk, s->T, keep)) return MODA_ERR_WORKSPACE;
+  moda::EvictParams p{};
+  p.K = (const char*)Kseq; p.V = (const char*)Vseq; p.w = weights; p.positions = positions; p.lengths = lengths;
+  p.K_out = (char*)Kout; p.V_out = (char*)Vout; p.w_out = weights_out; p.positions_out = positions_out;
+  p.lengths_out = lengths_out; p.index = index;
+  p.B = s->B; p.Hk = s->Hk; p.T = s->T; p.T_alloc = kv_alloc; p.out_alloc = out_alloc;
+  p.n = n; p.keep = keep; p.recent = recent;
+  p.row_bytes = s->d * (s->dtype == MODA_BF16 ? 2 : 4);
+  p.in_place = in_place;
+  return launch_status(moda::launch_evict(p, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
 size_t moda_calibrate_mfma_operand_bytes(void) { return moda::calibrate_operand_bytes(); }
 size_t moda_calibrate_mfma_sink_bytes(int32_t workgroups) {
   return workgroups > 0 ? moda::calibrate_sink_bytes(workgroups) : 0;

@@ -66,6 +66,72 @@ hipError_t launch_decode_bf16(const void* Q, const void* Kseq, const void* Vseq,
                               int Hk, int T, int T_alloc, int d, int depth_alloc, int depth_count, float scale,
                               hipStream_t stream);
 
+// Decoding step of sequences that share prefixes, ragged lengths, accumulated weights (moda_decode_shared.hip).
+struct SharedParams {
+  const void* Q;             // [B, Hq, d]
+  const void* Kp;            // [Np, Hk, P_alloc, d]
+  const void* Vp;
+  const void* Ks;            // [B, Hk, T_alloc, d]
+  const void* Vs;
+  const void* Kd;            // [B, Hk, depth_alloc, d]
+  const void* Vd;
+  const int* prefix_lengths;  // [Np] or null
+  const int* lengths;         // [B] or null
+  const float* w_in;          // [B, Hk, T_alloc] or null
+  float* w_out;               // the same, or null
+  void* O;
+  float* LSE;
+  float* ws;      // [B, Hq, n_slices, d + 2]
+  float* scores;  // [B, Hq, T] (with w_out)
+  int B, Hq, Hk, T, T_alloc;
+  int Np, P, P_alloc;
+  int depth_alloc, depth_count;
+  int n_prefix, prefix_per;  // slices of a prefix, rows of one
+  int n_own, own_per;        // slices of an own cache, rows of one
+  int n_slices;              // both, and one for the depth slots where there are any
+  float scale, scale_log2;
+};
+size_t decode_shared_workspace_bytes(const SharedParams& p, int d, bool with_weights);
+hipError_t launch_decode_shared(SharedParams p, int d, void* workspace, hipStream_t stream);
+
+// Attention weight gathered by every key of a prompt (moda_weights.hip).
+struct WeightsParams {
+  const void* Q;        // [B, Hq, T, d]
+  const void* K;        // [B, Hk, T_alloc, d]
+  const float* LSE;     // [B, Hq, T]
+  const int* lengths;   // [B] or null
+  const float* w_in;    // [B, Hk, T_alloc] or null
+  float* w_out;
+  int B, Hq, Hk, T, T_alloc;
+  int window;  // last queries that count (T or more: all)
+  int causal;
+  float scale_log2;
+};
+size_t weights_workspace_bytes(const WeightsParams& p, int d, bool f32);
+hipError_t launch_weights(const WeightsParams& p, int d, bool f32, void* workspace, hipStream_t stream);
+
+// Eviction from a sequence cache (moda_evict.hip).
+struct EvictParams {
+  const char* K;  // [B, Hk, T_alloc, row_bytes]
+  const char* V;
+  const float* w;        // [B, Hk, T_alloc]
+  const int* positions;  // [B, Hk, T_alloc] or null
+  const int* lengths;    // [B] or null
+  char* K_out;  // [B, Hk, out_alloc, row_bytes]
+  char* V_out;
+  float* w_out;        // [B, Hk, out_alloc]
+  int* positions_out;  // [B, Hk, out_alloc] or null
+  int* lengths_out;    // [B] or null
+  int* index;          // [B, Hk, n]
+  int B, Hk, T, T_alloc, out_alloc;
+  int n;     // min(keep, T)
+  int keep, recent;
+  int row_bytes;
+  bool in_place;
+};
+size_t evict_workspace_bytes(int B, int Hk, int T, int keep);
+hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t stream);
+
 // Matrix-pipe calibration kernel (moda_calibrate.hip).
 size_t calibrate_operand_bytes();
 size_t calibrate_sink_bytes(int workgroups);

@@ -1,0 +1,340 @@
+"""The decoding step over shared prefixes and ragged caches, with and without accumulated weights, against fp64.
+
+Tolerances.  Weights are rounded to bf16 once at most (matrix pipe) and O once: U (|O| + sum w |v|), U = 2^-8, with a
+quarter to spare for the fp32 sums.  A logit is a sum of d products in fp32: its error is at most e = (d + 8) 2^-24 times
+scale * sum |q_i k_i|; the LSE moves by as much, plus the fp32 sum of the exponentials (at most some hundred terms per
+lane: 5e-5).  A weight exp(x - LSE) moves by its share of both."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_ref as R
+from paper_2603_15619_amd import synth
+
+U = 2.0 ** -8
+f = synth.to_f64
+
+
+def tolerances(r, d):
+    e = (d + 8) * 2.0 ** -24 * r["logit"]
+    return 1.25 * U * (np.abs(r["O"]) + r["mag"]) + 1e-6, e + 5e-5 + 2.0 ** -21 * np.abs(np.where(np.isfinite(r["LSE"]), r["LSE"], 0))
+
+
+def inputs(B, Hq, Hk, T, d, L, P=0, Np=1, La=None, kv_alloc=None, prefix_alloc=None, seed=0, scale_q=1.0):
+    g = torch.Generator().manual_seed(seed)
+
+    def t(*shape):
+        return torch.randn(shape, generator=g).to(torch.bfloat16).cuda()
+
+    La = L if La is None else La
+    kv_alloc, prefix_alloc = kv_alloc or T, prefix_alloc or P
+    x = {"Q": (t(B, Hq, d) * scale_q).contiguous(), "Kprefix": t(Np, Hk, prefix_alloc, d) if prefix_alloc else None,
+         "Vprefix": t(Np, Hk, prefix_alloc, d) if prefix_alloc else None,
+         "Kseq": t(B, Hk, kv_alloc, d) if kv_alloc else None, "Vseq": t(B, Hk, kv_alloc, d) if kv_alloc else None,
+         "Kdepth": t(B, Hk, La, d) if La else None, "Vdepth": t(B, Hk, La, d) if La else None}
+    return x
+
+
+def poison(x, lens, plens, L, T):
+    """NaN where no value may be read."""
+    for name in ("Kseq", "Vseq"):
+        if x[name] is not None:
+            for b, n in enumerate(lens):
+                x[name][b, :, max(0, min(n, T)):] = float("nan")
+    for name in ("Kprefix", "Vprefix"):
+        if x[name] is not None:
+            for i, n in enumerate(plens):
+                x[name][i, :, n:] = float("nan")
+    for name in ("Kdepth", "Vdepth"):
+        if x[name] is not None:
+            x[name][:, :, L:] = float("nan")
+
+
+def ints(v):
+    return None if v is None else torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def up(x, *names):
+    return [None if x[n] is None else f(x[n]) for n in names]
+
+
+def check(B, Hq, Hk, T, d, L, P=0, Np=1, lens=None, plens=None, La=None, kv_alloc=None, prefix_alloc=None, seed=0,
+          scale=None, weights=True, scale_q=1.0, change=None):
+    from paper_2603_15619_amd import moda_attn_decode_shared
+
+    print("case", dict(B=B, Hq=Hq, Hk=Hk, T=T, d=d, L=L, P=P, Np=Np, lens=lens, plens=plens, seed=seed), flush=True)
+    x = inputs(B, Hq, Hk, T, d, L, P, Np, La, kv_alloc, prefix_alloc, seed, scale_q)
+    poison(x, lens or [T] * B, plens or [P] * Np, L, T)
+    if change:
+        change(x)
+    w_in = w_out = None
+    if weights and x["Kseq"] is not None:
+        w_in = torch.rand(x["Kseq"].shape[:3], device="cuda")
+        w_out = torch.full_like(w_in, -7.0)
+    out = torch.full_like(x["Q"], float("nan"))
+    lse = torch.full((B, Hq), float("nan"), device="cuda")
+    O, LSE = moda_attn_decode_shared(**x, prefix_lengths=ints(plens), lengths=ints(lens), P=P, T=T, depth_count=L, scale=scale,
+                                     weights=w_in, weights_out=w_out, out=out, lse=lse)
+    torch.cuda.synchronize()
+    r = R.decode_step(*(None if a is None else np.nan_to_num(a, nan=0.0, posinf=np.inf, neginf=-np.inf) for a in
+                        up(x, "Q", "Kprefix", "Vprefix", "Kseq", "Vseq", "Kdepth", "Vdepth")),
+                      plens, lens, P, T, L, scale)
+    to, tl = tolerances(r, d)
+    eo = np.abs(f(O) - r["O"]) / to
+    finite = np.isfinite(r["LSE"])
+    assert np.array_equal(finite, np.isfinite(f(LSE))) and np.all(f(LSE)[~finite] == -np.inf)
+    el = np.abs(f(LSE)[finite] - r["LSE"][finite]) / tl[finite]
+    print("   O %.3f LSE %.3f of the tolerance" % (eo.max(initial=0), el.max(initial=0)), flush=True)
+    assert np.all(eo <= 1) and np.all(el <= 1)
+    if w_out is not None:
+        G = Hq // Hk
+        rel = (2 * tl).reshape(B, Hk, G).max(-1)[:, :, None]
+        n = np.array([min(max(v, 0), T) for v in lens or [T] * B])
+        want = f(w_in) + r["weights"]
+        filled = np.arange(w_in.shape[2])[None, None, :] < n[:, None, None]
+        ew = np.abs(f(w_out) - want) / (rel * r["weights"] + (G + 2) * 2.0 ** -23 * want + 1e-9)
+        print("   weights %.3f of the tolerance" % np.where(filled, ew, 0).max(initial=0), flush=True)
+        assert np.all(np.where(filled, ew, 0) <= 1)
+        assert np.all(np.where(filled, -7.0, f(w_out)) == -7.0)  # rows behind a sequence: left as they were
+    return O, LSE, w_out
+
+
+SHAPES = [
+    dict(B=1, Hq=1, Hk=1, T=1, d=64, L=0),
+    dict(B=1, Hq=2, Hk=2, T=0, d=128, L=0, P=1),
+    dict(B=4, Hq=16, Hk=16, T=40, d=128, L=15, P=1003, La=16),
+    dict(B=3, Hq=6, Hk=2, T=33, d=64, L=1, P=257, kv_alloc=40, prefix_alloc=300),
+    dict(B=6, Hq=5, Hk=1, T=64, d=128, L=0, P=500, Np=3),
+    dict(B=33, Hq=8, Hk=1, T=70, d=64, L=31, P=1000),
+    dict(B=20, Hq=64, Hk=2, T=5, d=64, L=3, P=300, Np=2),
+    dict(B=9, Hq=8, Hk=8, T=31, d=128, L=7, P=2049),
+    dict(B=130, Hq=4, Hk=2, T=9, d=128, L=0, P=129),
+    dict(B=2, Hq=80, Hk=2, T=100, d=128, L=70, P=65),
+    dict(B=17, Hq=16, Hk=2, T=0, d=64, L=0, P=700, Np=17),
+    dict(B=40, Hq=16, Hk=2, T=20, d=128, L=4, P=96),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c", SHAPES)
+def test_shared_prefix(c):
+    check(**c, seed=len(str(c)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,Hq,Hk,T,d,L,lens", [
+    (5, 10, 10, 300, 128, 3, [0, 1, 299, 300, 128]), (4, 8, 2, 1000, 64, 0, [1000, 7, 0, 513]),
+    (3, 12, 1, 777, 128, 31, [777, -5, 900]),  # below zero counts as zero, above T as T
+    (2, 40, 1, 1537, 64, 15, [1537, 1025]), (2, 5, 1, 4100, 128, 7, [4100, 33]), (1, 1, 1, 20011, 64, 0, [20010]),
+    (7, 16, 2, 257, 64, 64, [256, 255, 257, 31, 32, 33, 0]), (2, 3, 1, 600, 64, 1, None), (2, 2, 1, 65, 128, 0, [65, 64])])
+def test_ragged_lengths_and_weights(B, Hq, Hk, T, d, L, lens):
+    check(B, Hq, Hk, T, d, L, lens=lens, kv_alloc=T + 5, seed=T + L)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,G", [(64, 1), (128, 1), (64, 8), (128, 8)])
+def test_ragged_prefixes_empty_ones_among_them(d, G):
+    check(8, 2 * G, 2, 50, d, 0, P=700, Np=4, lens=[0, 50, 3, 0, 0, 0, 1, 2], plens=[700, 0, 0, 33], prefix_alloc=704, seed=d + G)
+    check(12, 2 * G, 2, 0, d, 0, P=40, Np=3, plens=[0, 40, -3], seed=d + G, weights=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(16))
+def test_random_shapes(seed):
+    rng = np.random.default_rng(7700 + seed)
+    d, Hk, G = int(rng.choice([64, 128])), int(rng.integers(1, 4)), int(rng.choice([1, 2, 3, 4, 5, 7, 8, 9, 16, 33]))
+    Np, per = int(rng.integers(1, 4)), int(rng.integers(1, 12))
+    T, P, L = int(rng.integers(0, 600)), int(rng.integers(0, 1500)), int(rng.choice([0, 1, 5, 32, 33, 100]))
+    lens = rng.integers(0, T + 1, Np * per).tolist()
+    plens = rng.integers(0, P + 1, Np).tolist()
+    check(Np * per, G * Hk, Hk, T, d, L, P, Np, lens, plens, La=L + int(rng.integers(0, 4)), kv_alloc=T + int(rng.integers(1, 30)),
+          prefix_alloc=P + int(rng.integers(1, 30)), seed=7700 + seed)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [1, 8])
+def test_scale_and_large_logits(G):
+    """Logits of several hundred, both signs: references move by many powers of two between slices."""
+    check(4, 2 * G, 2, 700, 64, 5, P=900, lens=[700, 1, 0, 350], scale=0.5, scale_q=8.0, seed=3)
+    check(4, 2 * G, 2, 90, 128, 0, P=300, scale=2.0 ** -10, seed=4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [1, 2, 8])
+def test_infinite_values_reach_only_those_who_see_them(G):
+    """Sequence 1's own cache and prefix 1 hold infinite values: the other outputs stay finite."""
+    def change(x):
+        x["Vseq"][1, :, 3] = float("inf")
+        x["Vprefix"][1, :, 5] = float("inf")
+    from paper_2603_15619_amd import moda_attn_decode_shared
+
+    x = inputs(6, 2 * G, 2, 65, 128, 2, 77, 3, seed=5)
+    change(x)
+    O, LSE = moda_attn_decode_shared(**x)
+    assert torch.isfinite(LSE).all()
+    bad = torch.isinf(O).any(-1)
+    assert bad[1:4].all() and not bad[0].any() and not bad[4:].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [1, 8])
+def test_logits_of_minus_infinity_and_nan(G):
+    """A key whose logit is -inf weighs nothing; a sequence with no other key is one that sees nothing.  A NaN stays with
+    the sequences that see it."""
+    from paper_2603_15619_amd import moda_attn_decode_shared
+
+    x = inputs(3, 2 * G, 2, 40, 64, 0, seed=6)
+    x["Q"][:] = x["Q"].abs() + 0.1
+    x["Kseq"][0, :, 7] = float("-inf")
+    x["Kseq"][1] = float("-inf")
+    x["Kseq"][2, :, 9] = float("nan")
+    w = torch.zeros((3, 2, 40), device="cuda")
+    O, LSE = moda_attn_decode_shared(Q=x["Q"], Kprefix=None, Vprefix=None, Kseq=x["Kseq"], Vseq=x["Vseq"], weights=w)
+    assert torch.isfinite(O[0].float()).all() and (w[0, :, 7] == 0).all()
+    assert (O[1] == 0).all() and (LSE[1] == float("-inf")).all() and (w[1] == 0).all()
+    assert torch.isnan(O[2].float()).all() and torch.isnan(LSE[2]).all() and torch.isnan(w[2]).all()
+    keep = torch.arange(40, device="cuda") != 7
+    y = {k: x[k][:1, :, keep].contiguous() for k in ("Kseq", "Vseq")}
+    O1, L1 = moda_attn_decode_shared(x["Q"][:1].contiguous(), None, None, y["Kseq"], y["Vseq"])
+    assert (O1 - O[:1]).abs().max() <= 2 * U * O1.abs().max() and (L1 - LSE[:1]).abs().max() <= 1e-5
+
+
+@pytest.mark.gpu
+def test_agrees_with_the_plain_decoding_step():
+    """A prefix copied into every sequence's cache gives what sharing it gives."""
+    from paper_2603_15619_amd import moda_attn_decode, moda_attn_decode_shared
+
+    for G, d in ((1, 128), (4, 64), (8, 128)):
+        x = inputs(6, 2 * G, 2, 50, d, 5, 333, 2, seed=G)
+        O, LSE = moda_attn_decode_shared(**x)
+        K, V = (torch.cat([x[p].repeat_interleave(3, 0), x[s]], 2).contiguous() for p, s in (("Kprefix", "Kseq"), ("Vprefix", "Vseq")))
+        O2, L2 = moda_attn_decode(x["Q"], K, V, x["Kdepth"], x["Vdepth"])
+        # each is within U (|O| + sum w |v|) of the exact value; sum w |v| <= 5 here
+        assert (O.float() - O2.float()).abs().max() <= 2 * U * 5 and (LSE - L2).abs().max() <= 2e-4
+
+
+@pytest.mark.gpu
+def test_weights_in_place_from_zero_and_summing_to_the_heads():
+    from paper_2603_15619_amd import moda_attn_decode_weights
+
+    x = inputs(3, 12, 2, 200, 64, 0, seed=8)
+    lens = ints([200, 77, 0])
+    O, LSE, w = moda_attn_decode_weights(x["Q"], x["Kseq"], x["Vseq"], lengths=lens)
+    s = w.double().sum(-1)
+    assert (s[:2] - 6).abs().max() <= 1e-4 and (s[2] == 0).all() and (w[1, :, 77:] == 0).all()
+    w2 = w.clone()
+    O2, LSE2, w3 = moda_attn_decode_weights(x["Q"], x["Kseq"], x["Vseq"], w2, lengths=lens)
+    assert w3 is w2 and torch.equal(O, O2) and torch.equal(LSE, LSE2)
+    assert (w2 - 2 * w).abs().max() <= 2.0 ** -23 * 12
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    O4, _, w4 = moda_attn_decode_weights(x["Q"], x["Kseq"], x["Vseq"], lengths=lens, workspace=ws.fill_(255))
+    assert torch.equal(O, O4) and torch.equal(w, w4)  # what a workspace holds plays no part, and a call repeats to the bit
+
+
+@pytest.mark.gpu
+def test_captured_calls_and_streams():
+    """Two graphs with a workspace of their own, replayed in turn with eager calls between, on a stream of their own."""
+    from paper_2603_15619_amd import moda_attn_decode_shared
+
+    side = torch.cuda.Stream()
+    graphs = []
+    for G in (1, 8):
+        x = inputs(4, 2 * G, 2, 300, 128, 3, 800, 2, seed=20 + G)
+        w, lens = torch.zeros((4, 2, 300), device="cuda"), ints([300, 20, 0, 150])
+        out, lse = torch.empty_like(x["Q"]), torch.empty((4, 2 * G), device="cuda")
+        ws = torch.empty(1 << 23, dtype=torch.uint8, device="cuda")
+        w_in = torch.rand_like(w)
+        call = lambda: moda_attn_decode_shared(**x, lengths=lens, weights=w_in, weights_out=w, out=out, lse=lse, workspace=ws)
+        call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            call()
+        graphs.append((g, x, lens, w_in, w, out, lse))
+    for step in range(3):
+        for g, x, lens, w_in, w, out, lse in graphs:
+            x["Q"].copy_(torch.randn_like(x["Q"]))
+            lens.copy_(ints([300 - step, 20 + step, step, 150]))
+            w.zero_()
+            out.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            w2 = torch.zeros_like(w)
+            O, LSE = moda_attn_decode_shared(**x, lengths=lens, weights=w_in, weights_out=w2)
+            assert torch.equal(O, out) and torch.equal(LSE, lse) and torch.equal(w, w2)
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        _, x, lens, w_in, w, out, lse = graphs[0]
+        O, LSE = moda_attn_decode_shared(**x, lengths=lens)
+    side.synchronize()
+    assert torch.equal(O, out) and torch.equal(LSE, lse)
+
+
+# ---------------------------------------------------------------- refusals, on the host
+OK = dict(B=4, Hq=4, Hk=2, T=16, d=128, depth_alloc=3, depth_count=2, causal=1, scale=0.0, dtype=1)
+
+
+def status(shape=None, prefix=(2, 10, 12), kv_alloc=16, ws_bytes=1 << 40, null=(), bad=(), **more):
+    from paper_2603_15619_amd.binding import MODAPrefix, MODAShape, lib
+
+    names = ["Q", "Kp", "Vp", "Ks", "Vs", "Kd", "Vd", "plens", "lens", "w_in", "w_out", "O", "LSE", "ws"]
+    p = {n: ctypes.c_void_p(None if n in null else 0x1008 if n in bad else 0x1000) for n in names}
+    s = MODAShape(**dict(OK, **(shape or {})))
+    x = None if prefix is None else ctypes.byref(MODAPrefix(*prefix))
+    return lib().moda_attn_decode_shared(*(p[n] for n in names[:13]), kv_alloc, p["ws"], ws_bytes, x, ctypes.byref(s), None)
+
+
+def test_refusals_without_gpu():
+    from paper_2603_15619_amd.binding import MODAPrefix, MODAShape, lib
+
+    assert status(dict(B=0)) == 0
+    assert status(dict(dtype=0)) == 3 and status(dict(d=96)) == 3 and status(dict(Hq=5)) == 2
+    assert status(dict(depth_count=4)) == 2 and status(dict(T=-1)) == 2 and status(kv_alloc=15) == 2
+    assert status(prefix=(0, 10, 12)) == 2 and status(prefix=(3, 10, 12)) == 2  # B is no multiple of the prefixes
+    assert status(prefix=(2, 13, 12)) == 2 and status(prefix=(2, -1, 12)) == 2
+    for name in ("Q", "Kp", "Vp", "Ks", "Vs", "Kd", "Vd", "O", "LSE"):
+        assert status(null=[name]) == 1, name
+    assert status(null=["w_out"]) == 1  # weights_in without weights_out
+    for name in ("Q", "Kp", "Vp", "Ks", "Vs", "Kd", "Vd", "O", "LSE", "w_in", "w_out", "ws"):
+        assert status(bad=[name]) == 4, name
+    assert status(null=["ws"]) == 6
+    s, x = MODAShape(**OK), MODAPrefix(2, 10, 12)
+    need = [lib().moda_attn_decode_shared_workspace_bytes(ctypes.byref(x), w, ctypes.byref(s)) for w in (0, 1)]
+    assert 0 < need[0] < need[1]
+    assert status(ws_bytes=need[1] - 1) == 6 and status(ws_bytes=need[0] - 1, null=["w_in", "w_out"]) == 6
+    assert lib().moda_attn_decode_shared(*([None] * 13), 0, None, 0, None, None, None) == 1
+    assert status(dict(B=1 << 22, Hq=512, Hk=512), kv_alloc=16, prefix=None) == 3  # more heads than a launch has threads
+    p = ctypes.c_void_p(0x1000)
+    weights = lambda w, T=16: lib().moda_attn_decode_weights(p, p, p, p, p, p, p, w, p, p, T, p, 1, ctypes.byref(MODAShape(**OK)), None)
+    assert weights(None) == 1 and weights(p) == 6 and weights(p, 15) == 2
+
+
+def test_binding_refusals_without_gpu():
+    from paper_2603_15619_amd import moda_attn_decode_shared, moda_attn_decode_weights
+
+    t = torch.zeros(2, 4, 8, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device memory"):
+        moda_attn_decode_shared(t[:, :, 0].contiguous(), t, t, t, t)
+    with pytest.raises(ValueError, match="device memory"):
+        moda_attn_decode_weights(t[:, :, 0].contiguous(), t, t)
+    with pytest.raises(ValueError, match="Kseq or Kprefix"):
+        moda_attn_decode_shared(t[:, :, 0].contiguous(), None, None, None, None)
+
+
+@pytest.mark.gpu
+def test_binding_refusals():
+    from paper_2603_15619_amd import MODAError, moda_attn_decode_shared
+
+    x = inputs(4, 4, 2, 20, 64, 0, 10, 2, seed=1)
+    with pytest.raises(ValueError, match="contiguous"):
+        moda_attn_decode_shared(**dict(x, Kseq=x["Kseq"].transpose(0, 1).contiguous().transpose(0, 1)))
+    with pytest.raises(ValueError, match="lengths"):
+        moda_attn_decode_shared(**x, lengths=torch.zeros(4, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError, match="weights"):
+        moda_attn_decode_shared(**x, weights=torch.zeros(4, 2, 19, device="cuda"))
+    with pytest.raises(MODAError, match="shape"):
+        moda_attn_decode_shared(**x, T=21)
+    with pytest.raises(MODAError, match="workspace"):
+        moda_attn_decode_shared(**x, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
