@@ -82,11 +82,13 @@ struct SharedParams {
   void* O;
   float* LSE;
   float* ws;      // [B, Hq, n_slices, d + 2]
-  float* scores;  // [B, Hq, T] (with w_out)
+  float* scores;  // [B, Hq, score_step] (with w_out): logits of the own rows, before the scale
+  size_t score_step;
   int B, Hq, Hk, T, T_alloc;
   int Np, P, P_alloc;
   int depth_alloc, depth_count;
-  int n_prefix, prefix_per;  // slices of a prefix, rows of one
+  int prefix_kind, prefix_groups, prefix_blocks;  // how prefixes are read, workgroups per prefix, head and column chunk, in all
+  int n_prefix, prefix_per;  // states of a prefix, rows of a slice
   int n_own, own_per;        // slices of an own cache, rows of one
   int n_slices;              // both, and one for the depth slots where there are any
   float scale, scale_log2;
