@@ -1,7 +1,7 @@
 // Eviction from a sequence cache: which rows of a (sequence, key/value head) stay, and their move.
 //
 // choice : one workgroup per (sequence, head).  A row's rank is a 32-bit key that orders as its weight does (recent rows
-//          above everything else); the key of the last row that stays is found digit by digit from histograms, ties
+//          above everything else); the key of the last row that stays is found in three digits from histograms, ties
 //          are counted in row order.  Kept rows below the new length keep their row; the i-th kept row
 //          behind it takes the i-th hole below it.  Result: `index`, the row that every new row comes from.
 // move   : rows of K and V, weights and positions from index[r] to r.  In place, a moved row lies behind the new length
@@ -20,10 +20,15 @@ __device__ __forceinline__ unsigned weight_key(float w) {
   return w != w ? 0u : u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
+// Rows of a (sequence, head): wave w takes `steps` times 64 of them, from w * steps * 64 on.  N > 0: steps = N, and a row's key stays in
+// a register from its one read on; 0: as many steps as it takes, and every pass reads weights and positions again.
+template <int N>
 __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictParams p, int* movers_ws) {
-  __shared__ unsigned hist[256];
+  constexpr int kBins = 2048;
+  __shared__ unsigned hist[kBins];
   __shared__ int part[kEvWaves], part2[kEvWaves];
-  __shared__ int s_digit, s_need;
+  __shared__ unsigned s_digit;
+  __shared__ int s_need;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bg = blockIdx.x, b = bg / p.Hk;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
@@ -36,77 +41,129 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   }
   const float* w = p.w + (size_t)bg * p.T_alloc;
   const int* pos = p.positions ? p.positions + (size_t)bg * p.T_alloc : nullptr;
+  const int steps = N > 0 ? N : (len + kEvThreads - 1) / kEvThreads;
+  const int r0 = wave * steps * 64 + lane;  // the lane's rows: r0 + 64 i
+  unsigned keys[N > 0 ? N : 1];
+  // N > 0: bounds-checked loads from one address register; rows past the end read as 0
+  const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc((void*)w, 0, N > 0 ? len * 4 : 0, 0x00020000);
+  const __amdgpu_buffer_rsrc_t pos_buf = __builtin_amdgcn_make_buffer_rsrc((void*)pos, 0, N > 0 && pos ? len * 4 : 0, 0x00020000);
+  auto each = [&](auto&& f) {  // f(i) for every step
+    if constexpr (N > 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) f(i);
+    } else {
+      for (int i = 0; i < steps; ++i) f(i);
+    }
+  };
+
   long long above = 0x7fffffffLL;  // rows whose position is above this are recent
+  const bool by_position = p.recent > 0 && pos;
   if (p.recent > 0) {
     int newest = len - 1;
     if (pos) {
       newest = (int)0x80000000;
-      for (int r = tid; r < len; r += kEvThreads) newest = max(newest, pos[r]);
+      each([&](int i) {
+        int x;
+        if constexpr (N > 0) keys[i] = (unsigned)(x = __builtin_amdgcn_raw_buffer_load_b32(pos_buf, r0 * 4, i * 256, 0));
+        else x = pos[min(r0 + i * 64, len - 1)];
+        if (r0 + i * 64 < len) newest = max(newest, x);
+      });
 #pragma unroll
       for (int x = 1; x < 64; x *= 2) newest = max(newest, __shfl_xor(newest, x));
       if (lane == 0) part[wave] = newest;
       __syncthreads();
+#pragma unroll
       for (int i = 0; i < kEvWaves; ++i) newest = max(newest, part[i]);
       __syncthreads();
     }
     above = (long long)newest - p.recent;
   }
-  auto key_of = [&](int r) { return (long long)(pos ? pos[r] : r) > above ? 0xffffffffu : weight_key(w[r]); };
+  auto make_key = [&](int i) {
+    if constexpr (N > 0) {
+      const int at = by_position ? (int)keys[i] : r0 + i * 64;
+      const unsigned k = weight_key(__builtin_bit_cast(float, (unsigned)__builtin_amdgcn_raw_buffer_load_b32(w_buf, r0 * 4, i * 256, 0)));
+      return at > above ? 0xffffffffu : k;
+    } else {
+      const int r = min(r0 + i * 64, len - 1);
+      const unsigned k = weight_key(w[r]);
+      return (by_position ? pos[r] : r) > above ? 0xffffffffu : k;
+    }
+  };
+  if constexpr (N > 0) each([&](int i) { keys[i] = make_key(i); });
+  auto key_of = [&](int i) { return N > 0 ? keys[N > 0 ? i : 0] : make_key(i); };
 
-  // the key of the fit-th row from the top, and how many of the rows with just that key stay
+  // the key of the fit-th row from the top, and how many of the rows with just that key stay: 11, 11 and 10 bits
   unsigned threshold = 0;
   int need = fit;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+  auto digit = [&](int shift) {
+    const unsigned mask = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
+    for (int i = tid; i < kBins; i += kEvThreads) hist[i] = 0;
     __syncthreads();
-    const unsigned mask = shift == 24 ? 0u : ~0u << (shift + 8);
-    for (int r = tid; r < len; r += kEvThreads) {
-      const unsigned k = key_of(r);
-      if ((k & mask) == threshold) atomicAdd(&hist[(k >> shift) & 255], 1u);
+    each([&](int i) {
+      const unsigned k = key_of(i);
+      const bool in = r0 + i * 64 < len && (k & mask) == threshold;
+      const unsigned bin = (k >> shift) & (kBins - 1);
+      // many rows share a digit (equal weights, recent rows): those that share the first lane's are counted at once
+      const unsigned long long in_all = __ballot(in);
+      if (in_all) {
+        const unsigned lead = __builtin_amdgcn_readlane(bin, __builtin_ctzll(in_all));
+        const unsigned long long same = __ballot(in && bin == lead);
+        if (in && bin != lead) atomicAdd(&hist[bin], 1u);
+        if (lane == 0) atomicAdd(&hist[lead], (unsigned)__popcll(same));
+      }
+    });
+    __syncthreads();
+    // thread t: bins 2047 - 2 t and 2046 - 2 t; `sum` = rows in the bins of threads up to this one
+    const int hi = (int)hist[kBins - 1 - 2 * tid], both = hi + (int)hist[kBins - 2 - 2 * tid];
+    int sum = both;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+      const int y = __shfl_up(sum, x);
+      if (lane >= x) sum += y;
+    }
+    if (lane == 63) part[wave] = sum;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) sum += part[i];
+    const int before = sum - both;
+    if (before < need && sum >= need) {  // (one thread)
+      const bool first = need - before <= hi;
+      s_digit = kBins - 1 - 2 * tid - (first ? 0 : 1);
+      s_need = need - before - (first ? 0 : hi);
     }
     __syncthreads();
-    if (tid == 0) {
-      int left = need, digit = 255;
-      while (left > (int)hist[digit]) left -= hist[digit--];
-      s_digit = digit;
-      s_need = left;
-    }
-    __syncthreads();
-    threshold |= (unsigned)s_digit << shift;
+    threshold |= s_digit << shift;
     need = s_need;
-    __syncthreads();
-  }
+  };
+  digit(21);
+  digit(10);
+  digit(0);
 
-  // a wave takes a stretch of rows, 64 at a time
-  const int stretch = (len + kEvThreads - 1) / kEvThreads * 64;
-  const int r0 = wave * stretch, r1 = min(len, r0 + stretch);
   const unsigned long long below = (1ull << lane) - 1;
-  auto before = [&](int* counts) {  // sum over the waves before this one
+  auto before = [&](const int* counts) {  // sum over the waves before this one
     int n = 0;
     for (int i = 0; i < wave; ++i) n += counts[i];
     return n;
   };
   int ties = 0;
-  for (int base = r0; base < r1; base += 64)
-    ties += __popcll(__ballot(base + lane < r1 && key_of(base + lane) == threshold));
+  each([&](int i) { ties += __popcll(__ballot(r0 + i * 64 < len && key_of(i) == threshold)); });
   if (lane == 0) part[wave] = ties;
   __syncthreads();
   const int ties_before = before(part);
   __syncthreads();
-  auto walk = [&](auto&& f) {  // f(row, stays) for every row of the stretch, all lanes
+  auto walk = [&](auto&& f) {  // f(row, stays) for every row, in order, all lanes
     int seen = ties_before;
-    for (int base = r0; base < r1; base += 64) {
-      const int r = base + lane;
-      const unsigned k = r < r1 ? key_of(r) : 0u;
-      const unsigned long long tie = __ballot(r < r1 && k == threshold);
+    each([&](int i) {
+      const int r = r0 + i * 64;
+      const unsigned k = key_of(i);
+      const unsigned long long tie = __ballot(r < len && k == threshold);
       const bool is_tie = (tie >> lane) & 1;
-      f(r, r < r1 && (is_tie ? seen + __popcll(tie & below) < need : k > threshold));
+      f(r, r < len && (is_tie ? seen + __popcll(tie & below) < need : k > threshold));
       seen += __popcll(tie);
-    }
+    });
   };
   int holes = 0, movers = 0;
   walk([&](int r, bool stays) {
-    holes += __popcll(__ballot(r < fit && r < r1 && !stays));
+    holes += __popcll(__ballot(r < fit && !stays));
     movers += __popcll(__ballot(r >= fit && stays));
   });
   if (lane == 0) {
@@ -124,8 +181,8 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   __syncthreads();
   nth = before(part);
   walk([&](int r, bool stays) {
-    const unsigned long long ho = __ballot(r < fit && r < r1 && !stays);
-    if (r < fit && r < r1) index[r] = stays ? r : list[nth + __popcll(ho & below)];
+    const unsigned long long ho = __ballot(r < fit && !stays);
+    if (r < fit) index[r] = stays ? r : list[nth + __popcll(ho & below)];
     nth += __popcll(ho);
   });
 }
@@ -159,7 +216,11 @@ hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t strea
   const int per_row = p.row_bytes / 16;
   const long long chunks = ((long long)p.n * per_row + 255) / 256;
   if (!grid_ok(groups, kEvThreads) || chunks > 0x7fffffff || !grid_ok(groups * chunks, 256)) return kGridTooLarge;
-  const hipError_t e = launch_kernel(moda_evict_choose_kernel, dim3((unsigned)groups), dim3(kEvThreads), stream, p, (int*)workspace);
+  auto* choose = p.T <= 1 * kEvThreads ? moda_evict_choose_kernel<1> : p.T <= 2 * kEvThreads ? moda_evict_choose_kernel<2>
+                 : p.T <= 4 * kEvThreads ? moda_evict_choose_kernel<4> : p.T <= 8 * kEvThreads ? moda_evict_choose_kernel<8>
+                 : p.T <= 16 * kEvThreads ? moda_evict_choose_kernel<16> : p.T <= 32 * kEvThreads ? moda_evict_choose_kernel<32>
+                 : moda_evict_choose_kernel<0>;
+  const hipError_t e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p, (int*)workspace);
   if (e != hipSuccess) return e;
   return launch_kernel(moda_evict_move_kernel, dim3((unsigned)(groups * chunks)), dim3(256), stream, p, per_row, (int)chunks);
 }
