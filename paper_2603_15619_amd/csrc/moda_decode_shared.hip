@@ -5,13 +5,13 @@
 //     m = max x,  l = sum exp(x_c - m),  O = (1/l) sum exp(x_c - m) v_c,  LSE = m + ln l,
 //     weights_out[j] = weights_in[j] + sum over the heads of a group of exp(x_j - LSE).
 // (m, l, unnormalised O) of disjoint sets of rows merge exactly, so the rows are cut into slices over workgroups, whose
-// states go to the workspace in fp32, and a second kernel merges them.  Where weights are asked for, the own
-// rows' logits go there too (4 bytes per row and head, where a row of K and V is 4 d), since no slice knows the LSE.
+// states go to the workspace in fp32, and a second kernel merges them.  Where weights are asked for, the own rows' logits go
+// there too (4 bytes per row and head, where a row of K and V is 4 d bytes), since no slice knows the LSE.
 //
 // One launch takes all slices:
 //   prefixes   all queries that share a prefix (sequences x heads of a group) are the columns of matrix products
-//              S^T = K Q^T, O^T += V^T P^T.  Up to 32 columns (read_by_wave): every wave has a slice of its own.  More
-//              (read_by_workgroup): 2 or 4 waves of 32 columns share the K and V tiles of a slice in LDS.
+//              S^T = K Q^T, O^T += V^T P^T.  Up to 32 columns (read_by_wave): every wave reads its own part of the slice.
+//              More (read_by_workgroup): 2 or 4 waves of 32 columns share the K and V tiles of a slice in LDS.
 //   own rows   up to 4 heads per group on the vector ALUs (read_rows), more as the columns of read_by_wave.
 #include <algorithm>
 
@@ -242,20 +242,56 @@ struct Columns {
                             pb, o[cb]);
       }
   }
-  // The lane's column to `dst` (null: a column past the last query).
-  __device__ __forceinline__ void store(float* dst, int hi) const {
-    const float l_all = pair_sum(l);
-    if (!dst) return;
-#pragma unroll
-    for (int cb = 0; cb < Tl::kDBlocks; ++cb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *(f32x4*)(dst + cb * 32 + i * 8 + hi * 4) = (f32x4){o[cb][4 * i], o[cb][4 * i + 1], o[cb][4 * i + 2], o[cb][4 * i + 3]};
-    if (hi == 0) *(f32x2*)(dst + D) = (f32x2){m, l_all};
-  }
 };
 
-// Every wave by itself: n rows at K and V (a slice of its own), 32 at a time through its two LDS tiles at `lds`; the next
+// The states of a workgroup's waves, those with the same columns (wave % CW) folded, to column -> dst(column) (null: a column
+// past the last query).  LDS: a wave's O^T as 16-byte pieces of four channels, piece c of column q at 32 c + (q ^ c % 32) of
+// the wave's part, so that both the writes (32 columns of a piece) and the reads (the pieces of a column, which make
+// whole rows in memory) touch every bank alike.
+template <int D, int CW, class Dst>
+__device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* smem, float (*stat)[32][2], float c2, Dst&& dst) {
+  constexpr int KW = kShWaves / CW, kPieces = D / 4, kPart = 32 * D * 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hi = lane >> 5;
+  const float l_all = pair_sum(c.l);
+  __syncthreads();  // (the tiles are not read any more)
+#pragma unroll
+  for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int piece = cb * 8 + i * 2 + hi;
+      *(f32x4*)(smem + wave * kPart + (piece * 32 + (l32 ^ (piece & 31))) * 16) =
+          (f32x4){c.o[cb][4 * i], c.o[cb][4 * i + 1], c.o[cb][4 * i + 2], c.o[cb][4 * i + 3]};
+    }
+  if (hi == 0) {
+    stat[wave][l32][0] = c.m;
+    stat[wave][l32][1] = l_all;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = tid; i < CW * 32 * kPieces; i += kShWaves * 64) {
+    const int col = i / kPieces, piece = i % kPieces, cw = col / 32, q = col % 32;
+    float* to = dst(col);
+    if (!to) continue;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KW; ++k) m = fmaxf(m, stat[k * CW + cw][q][0]);
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      const int w = k * CW + cw;
+      // (a lone wave's state as it is: its reference may be NaN, which the maximum leaves out)
+      const float f = KW == 1 ? 1.f : stat[w][q][0] == -INFINITY ? 0.f : fast_exp2((stat[w][q][0] - m) * c2);
+      l += f * stat[w][q][1];
+      const f32x4 x = *(const f32x4*)(smem + w * kPart + (piece * 32 + (q ^ (piece & 31))) * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+    }
+    *(f32x4*)(to + piece * 4) = o;
+    if (piece == 0) *(f32x2*)(to + D) = (f32x2){m, l};
+  }
+}
+
+// Every wave by itself: n rows at K and V (its part of the slice), 32 at a time through its two LDS tiles at `lds`; the next
 // block(s) are in flight in registers.  Rows past the end read as zeros (bounds-checked buffers) and fetch nothing.
 constexpr int waves_ahead(int d) { return d == 64 ? 2 : 1; }  // (d = 128: registers for one)
 template <int D>
@@ -348,110 +384,206 @@ constexpr int slices_lds() {
 template <int D, int PREFIX, int OWN>
 __global__ __launch_bounds__(kShWaves * 64, 2) void moda_shared_slices_kernel(SharedParams p) {
   constexpr int RB = D * 2;
+  constexpr bool kMatrix = PREFIX > 0 || OWN == 0;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[slices_lds<D, PREFIX, OWN>()];
+  __shared__ float stat[kMatrix ? kShWaves : 1][32][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, hi = lane >> 5;
   const unsigned lds = (unsigned)(size_t)(lds_ptr)smem;
   const int G = p.Hq / p.Hk;
   const float c2 = p.scale_log2;
   const size_t state = (size_t)p.n_slices * state_floats(D);  // of one head
   int id = blockIdx.x;
+  // a wave's part of the n rows of a slice: a quarter, in whole blocks of 32
+  auto part = [&](int n, int& first) {
+    const int q = ((n + kShWaves - 1) / kShWaves + 31) / 32 * 32;
+    first = min(wave * q, n);
+    return min(q, n - first);
+  };
   if (PREFIX > 0 && id < p.prefix_blocks) {
     const int per = p.B / p.Np, M = per * G;  // queries of a prefix and key/value head
-    constexpr int kCols = PREFIX * 32, KW = kShWaves / (PREFIX > 0 ? PREFIX : 1);
+    constexpr int CW = PREFIX > 0 ? PREFIX : 1, kCols = CW * 32;
     // column chunks of the same rows are neighbours on a die (ids equal mod 8), whose L2 then serves all but the first
     const int n_cc = (M + kCols - 1) / kCols;
     const int u = id / (8 * n_cc) * 8 + id % 8, cc = id / 8 % n_cc;
-    const int sg = u % p.prefix_groups, xg = u / p.prefix_groups;
+    const int slice = u % p.n_prefix, xg = u / p.n_prefix;
     if (xg >= p.Np * p.Hk) return;  // (padding of the grid; uniform)
     const int x = xg / p.Hk, g = xg - x * p.Hk;
     const int plen = filled(p.prefix_lengths, x, p.P);
     // column -> (sequence of the prefix, head of the group); a column past the last repeats it and is not stored
-    const int col = cc * kCols + (PREFIX == 4 ? wave : PREFIX == 2 ? (wave & 1) : 0) * 32 + l32;
-    const int cq = min(col, M - 1), seq = x * per + cq / G, h = g * G + cq % G;
-    const size_t bh = (size_t)seq * p.Hq + h;
-    const bool idle = col - l32 >= M;
+    auto head_of = [&](int col) { return (size_t)(x * per + col / G) * p.Hq + g * G + col % G; };
+    const int col0 = cc * kCols + (wave % CW) * 32;
     Columns<D> c;
-    c.init((const char*)p.Q + bh * RB, hi);
-    // PREFIX 1: each wave a slice.  Else: one slice per workgroup, KW interleaved parts of it per wave.
-    const int slice = PREFIX == 1 ? sg * kShWaves + wave : sg;
+    c.init((const char*)p.Q + head_of(min(col0 + l32, M - 1)) * RB, hi);
     const int begin = slice * p.prefix_per, n = max(0, min(plen - begin, p.prefix_per));
     const size_t at = ((size_t)xg * p.P_alloc + begin) * RB;
     const char *K = (const char*)p.Kp + at, *V = (const char*)p.Vp + at;
-    int part;
     if constexpr (PREFIX == 1) {
-      if (slice >= p.n_prefix) return;
-      read_by_wave<D>(c, K, V, n, lds + wave * 2 * 32 * RB, c2, nullptr);
-      part = slice;
+      int first;
+      const int mine = part(n, first);
+      read_by_wave<D>(c, K + (size_t)first * RB, V + (size_t)first * RB, mine, lds + wave * 2 * 32 * RB, c2, nullptr);
     } else {
-      read_by_workgroup<D, KW>(c, idle, K, V, n, lds, c2);
-      part = slice * KW + (KW == 2 ? wave >> 1 : 0);
+      read_by_workgroup<D, kShWaves / CW>(c, col0 >= M, K, V, n, lds, c2);
     }
-    c.store(col < M ? p.ws + bh * state + (size_t)part * state_floats(D) : nullptr, hi);
+    fold_waves<D, CW>(c, smem, stat, c2, [&](int col) {
+      col += cc * kCols;
+      return col < M ? p.ws + head_of(col) * state + (size_t)slice * state_floats(D) : nullptr;
+    });
     return;
   }
   if (PREFIX > 0) id -= p.prefix_blocks;
   // own rows: slices, then the depth slots
   const int n_own = p.n_slices - p.n_prefix;
-  constexpr int kHeads = OWN > 0 ? OWN : 32, kSlices = OWN > 0 ? 1 : kShWaves;  // of a workgroup
-  const int n_sg = (n_own + kSlices - 1) / kSlices, n_gc = (G + kHeads - 1) / kHeads;
-  const int sg = id % n_sg;
-  id /= n_sg;
+  constexpr int kHeads = OWN > 0 ? OWN : 32;  // of a workgroup
+  const int slice = id % n_own, n_gc = (G + kHeads - 1) / kHeads;
+  id /= n_own;
   const int gc = id % n_gc, bg = id / n_gc, b = bg / p.Hk, g = bg - b * p.Hk;
   const int h0 = g * G + gc * kHeads, nh = min(kHeads, G - gc * kHeads);
-  const int slice = sg * kSlices + (OWN > 0 ? 0 : wave);
   const bool depth = slice == p.n_own;
   const int begin = depth ? 0 : slice * p.own_per;
   const int n = depth ? p.depth_count : max(0, min(filled(p.lengths, b, p.T) - begin, p.own_per));
   const size_t at = ((size_t)bg * (depth ? p.depth_alloc : p.T_alloc) + begin) * RB;
   const char *K = (const char*)(depth ? p.Kd : p.Ks) + at, *V = (const char*)(depth ? p.Vd : p.Vs) + at;
   const size_t bh = (size_t)b * p.Hq + h0;
+  float* dst = p.ws + bh * state + (size_t)(p.n_prefix + slice) * state_floats(D);
   const bool keep = p.w_out && !depth;
   if constexpr (OWN > 0) {
-    read_rows<D, OWN>(K, V, n, (const char*)p.Q + bh * RB, nh, c2, p.ws + bh * state + (size_t)(p.n_prefix + slice) * state_floats(D), state,
-                      keep ? p.scores + bh * p.score_step + begin : nullptr, p.score_step, (float*)smem);
+    read_rows<D, OWN>(K, V, n, (const char*)p.Q + bh * RB, nh, c2, dst, state, keep ? p.scores + bh * p.score_step + begin : nullptr,
+                      p.score_step, (float*)smem);
   } else {
-    if (slice >= n_own) return;
     Columns<D> c;
-    const size_t mine = bh + min(l32, nh - 1);
-    c.init((const char*)p.Q + mine * RB, hi);
-    read_by_wave<D>(c, K, V, n, lds + wave * 2 * 32 * RB, c2, keep && l32 < nh ? p.scores + mine * p.score_step + begin : nullptr);
-    c.store(l32 < nh ? p.ws + mine * state + (size_t)(p.n_prefix + slice) * state_floats(D) : nullptr, hi);
+    const int j = min(l32, nh - 1);
+    c.init((const char*)p.Q + (bh + j) * RB, hi);
+    int first;
+    const int mine = part(n, first);
+    read_by_wave<D>(c, K + (size_t)first * RB, V + (size_t)first * RB, mine, lds + wave * 2 * 32 * RB, c2,
+                    keep && l32 < nh ? p.scores + (bh + j) * p.score_step + begin + first : nullptr);
+    fold_waves<D, 1>(c, smem, stat, c2, [&](int col) { return col < nh ? dst + col * state : nullptr; });
   }
 }
 
-// Thread = channel of one (batch, query head): folds its slices.
+// ---------------------------------------------------------------- outputs
+// Workgroups [0, merge_blocks): O and LSE.  `by` slices of a head at a time, D / 4 threads each (four channels a thread), 1024 / D
+// such teams in a workgroup.  The others: weights_out of 1024 rows of one (batch, key/value head); each finds the LSE of
+// the group's heads from the slices' references and normalisers (8 bytes of a state).
+constexpr int kFinishRows = 1024, kFinishHeads = 64;
 template <int D>
-__global__ __launch_bounds__(D) void moda_shared_merge_kernel(SharedParams p) {
-  const int ch = threadIdx.x, bh = blockIdx.x;
+__global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p, int by, int merge_blocks, int n_chunks) {
+  constexpr int kTeam = D / 4, kTeams = 256 / kTeam;
+  __shared__ __attribute__((aligned(16))) float red[kTeams][state_floats(D)];
   const float c2 = p.scale_log2;
-  const float* ws = p.ws + (size_t)bh * p.n_slices * state_floats(D);
-  float mm = -INFINITY, ll = 0.f, oo = 0.f;
-  for (int s = 0; s < p.n_slices; ++s) {
-    const float* w = ws + (size_t)s * state_floats(D);
-    const float mn = fmaxf(mm, w[D]);
-    const float al = mm == -INFINITY ? 0.f : fast_exp2((mm - mn) * c2), f = w[D] == -INFINITY ? 0.f : fast_exp2((w[D] - mn) * c2);
-    mm = mn;
-    ll = ll * al + f * w[D + 1];
-    oo = oo * al + f * w[ch];
+  const int tid = threadIdx.x;
+  // (a state whose scores are all -inf is empty: reference -inf, weight zero)
+  auto factor = [&](float m, float ref) { return m == -INFINITY ? 0.f : fast_exp2((m - ref) * c2); };
+  if ((int)blockIdx.x < merge_blocks) {
+    const int team = tid / kTeam, ch = tid % kTeam * 4, part = team % by;
+    const long long bh = (long long)blockIdx.x * (kTeams / by) + team / by, heads = (long long)p.B * p.Hq;
+    float mm = -INFINITY, ll = 0.f;
+    f32x4 oo = {0.f, 0.f, 0.f, 0.f};
+    const float* ws = p.ws + (size_t)min(bh, heads - 1) * p.n_slices * state_floats(D);
+    constexpr int kU = 4;
+    for (int s0 = part; s0 < p.n_slices; s0 += kU * by) {
+      f32x2 st[kU];
+      f32x4 o[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const float* x = ws + (size_t)min(s0 + u * by, p.n_slices - 1) * state_floats(D);
+        st[u] = *(const f32x2*)(x + D);
+        o[u] = *(const f32x4*)(x + ch);
+      }
+      float mn = mm;
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (s0 + u * by < p.n_slices) mn = fmaxf(mn, st[u][0]);
+      const float al = factor(mm, mn);
+      mm = mn;
+      ll *= al;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) oo[j] *= al;
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (s0 + u * by < p.n_slices) {
+          const float f = factor(st[u][0], mm);
+          ll += f * st[u][1];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) oo[j] += f * o[u][j];
+        }
+    }
+    if (by > 1) {  // (uniform)
+      *(f32x4*)&red[team][ch] = oo;
+      if (ch == 0) *(f32x2*)&red[team][D] = (f32x2){mm, ll};
+      __syncthreads();
+      if (part > 0) return;
+      const float m0 = mm;
+      for (int k = 1; k < by; ++k) mm = fmaxf(mm, red[team + k][D]);
+      const float f0 = factor(m0, mm);
+      ll *= f0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) oo[j] *= f0;
+      for (int k = 1; k < by; ++k) {
+        const float f = factor(red[team + k][D], mm);
+        ll += f * red[team + k][D + 1];
+        const f32x4 x = *(const f32x4*)&red[team + k][ch];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) oo[j] += f * x[j];
+      }
+    }
+    if (bh >= heads) return;
+    const bool none = ll == 0.f;  // nothing seen, or nothing that has weight
+    const float inv = none ? 0.f : 1.f / ll;
+    *(u32x2*)((__bf16*)p.O + bh * D + ch) = none ? (u32x2){0u, 0u} : (u32x2){pack_bf16(oo[0] * inv, oo[1] * inv), pack_bf16(oo[2] * inv, oo[3] * inv)};
+    if (ch == 0) p.LSE[bh] = none ? -INFINITY : mm * p.scale + __logf(ll);
+    return;
   }
-  const bool none = ll == 0.f;  // nothing seen, or nothing that has weight
-  ((__bf16*)p.O)[(size_t)bh * D + ch] = (__bf16)(none ? 0.f : oo / ll);
-  if (ch == 0) p.LSE[bh] = none ? -INFINITY : mm * p.scale + __logf(ll);
-}
-
-// weights_out = weights_in + the heads' weights: thread = row of one (batch, key/value head).
-__global__ __launch_bounds__(256) void moda_shared_weights_kernel(SharedParams p, int n_chunks) {
-  const int bg = blockIdx.x / n_chunks, j = (blockIdx.x % n_chunks) * 256 + threadIdx.x;
-  const int b = bg / p.Hk, g = bg - b * p.Hk, G = p.Hq / p.Hk;
-  if (j >= filled(p.lengths, b, p.T)) return;
-  const size_t at = (size_t)bg * p.T_alloc + j;
-  float w = p.w_in ? p.w_in[at] : 0.f;
-  for (int h = 0; h < G; ++h) {
-    const size_t bh = (size_t)b * p.Hq + g * G + h;
-    const float lse = p.LSE[bh];
-    if (lse != -INFINITY) w += fast_exp2(p.scores[bh * p.score_step + j] * p.scale_log2 - lse * 1.4426950408889634f);
+  const int id = blockIdx.x - merge_blocks, bg = id / n_chunks, j0 = id % n_chunks * kFinishRows;
+  const int b = bg / p.Hk, g = bg - b * p.Hk, G = p.Hq / p.Hk, lane = tid & 63;
+  const int len = filled(p.lengths, b, p.T);
+  if (j0 >= len) return;
+  constexpr int kRows = kFinishRows / 256;
+  const size_t row = (size_t)bg * p.T_alloc;
+  float w[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    const int j = min(j0 + i * 256 + tid, len - 1);
+    w[i] = p.w_in ? p.w_in[row + j] : 0.f;
   }
-  p.w_out[at] = w;
+  float* lse2 = &red[0][0];  // LSE * log2(e) of kFinishHeads heads; +inf where nothing has weight
+  static_assert(kFinishHeads <= kTeams * state_floats(D), "");
+  for (int h0 = 0; h0 < G; h0 += kFinishHeads) {
+    const int nh = min(kFinishHeads, G - h0);
+    __syncthreads();
+    for (int h = tid >> 6; h < nh; h += 4) {  // a wave per head
+      const float* ws = p.ws + ((size_t)b * p.Hq + g * G + h0 + h) * p.n_slices * state_floats(D) + D;
+      float m = -INFINITY, l = 0.f;
+      for (int s = lane; s < p.n_slices; s += 64) {
+        const f32x2 x = *(const f32x2*)(ws + (size_t)s * state_floats(D));
+        const float mn = fmaxf(m, x[0]);
+        l = l * factor(m, mn) + factor(x[0], mn) * x[1];
+        m = mn;
+      }
+#pragma unroll
+      for (int x = 1; x < 64; x *= 2) {
+        const float m2 = __shfl_xor(m, x), l2 = __shfl_xor(l, x), mn = fmaxf(m, m2);
+        l = l * factor(m, mn) + l2 * factor(m2, mn);
+        m = mn;
+      }
+      if (lane == 0) lse2[h] = l == 0.f ? INFINITY : m * c2 + __log2f(l);
+    }
+    __syncthreads();
+    const float* sc = p.scores + ((size_t)b * p.Hq + g * G + h0) * p.score_step;
+    for (int h = 0; h < nh; ++h) {
+      const float z = lse2[h];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const int j = min(j0 + i * 256 + tid, len - 1);
+        w[i] += fast_exp2(__builtin_fmaf(sc[h * p.score_step + j], c2, -z));
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    const int j = j0 + i * 256 + tid;
+    if (j < len) p.w_out[row + j] = w[i];
+  }
 }
 
 // ---------------------------------------------------------------- the cut into slices
@@ -468,26 +600,18 @@ static void plan(SharedParams& p) {
   };
   // prefixes: two workgroups of four waves per compute unit
   p.prefix_kind = p.P == 0 ? 0 : M <= 32 ? 1 : M <= 64 ? 2 : 4;
-  p.prefix_groups = p.n_prefix = p.prefix_per = 0;
+  p.n_prefix = p.prefix_per = 0;
   long long blocks = 0;
   if (p.P > 0) {
     const long long xg = (long long)p.Np * p.Hk, cc = (M + p.prefix_kind * 32 - 1) / (p.prefix_kind * 32);
-    int n;
-    if (p.prefix_kind == 1) {
-      cut(p.P, std::max(1ll, 2048 / xg), 128, 32, n, p.prefix_per);
-      p.n_prefix = n;
-      p.prefix_groups = (n + kShWaves - 1) / kShWaves;
-    } else {
-      cut(p.P, std::max(1ll, 512 / (xg * cc)), 256, 64, n, p.prefix_per);
-      p.n_prefix = n * (kShWaves / p.prefix_kind);
-      p.prefix_groups = n;
-    }
-    blocks = (xg * p.prefix_groups + 7) / 8 * 8 * cc;
+    if (p.prefix_kind == 1) cut(p.P, std::max(1ll, 768 / xg), 128, 128, p.n_prefix, p.prefix_per);
+    else cut(p.P, std::max(1ll, 512 / (xg * cc)), 256, 64, p.n_prefix, p.prefix_per);
+    blocks = (xg * p.n_prefix + 7) / 8 * 8 * cc;
   }
   p.prefix_blocks = blocks > 0x7fffffff ? 0x7fffffff : (int)blocks;  // (too many: the launch is refused)
   const long long groups = (long long)p.B * p.Hk;
   if (own_kind(G) > 0) cut(p.T, std::max(1ll, 2048 / groups), 256, 64, p.n_own, p.own_per);
-  else cut(p.T, std::max(1ll, 3072 / (groups * ((G + 31) / 32))), 128, 32, p.n_own, p.own_per);
+  else cut(p.T, std::max(1ll, 768 / (groups * ((G + 31) / 32))), 128, 128, p.n_own, p.own_per);
   p.n_slices = p.n_prefix + p.n_own + (p.depth_count > 0 ? 1 : 0);
   p.score_step = ((size_t)p.T + 31) / 32 * 32;
 }
@@ -512,24 +636,23 @@ static void (*slices_kernel(int own))(SharedParams) {
 template <int D>
 static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
   const int G = p.Hq / p.Hk, own = own_kind(G), n_own = p.n_slices - p.n_prefix;
-  const int heads_per = own > 0 ? own : 32, slices_per = own > 0 ? 1 : kShWaves;
-  const long long blocks = p.prefix_blocks + (long long)p.B * p.Hk * ((G + heads_per - 1) / heads_per) * ((n_own + slices_per - 1) / slices_per);
-  const long long heads = (long long)p.B * p.Hq;
-  const int chunks = (p.T + 255) / 256;
-  const long long w_blocks = (long long)p.B * p.Hk * chunks;
-  const bool weights = p.w_out && p.T > 0;
-  if ((blocks > 0 && !grid_ok(blocks, kShWaves * 64)) || !grid_ok(heads, D) || (weights && !grid_ok(w_blocks, 256)))
-    return kGridTooLarge;
-  hipError_t e = hipSuccess;
+  const int heads_per = own > 0 ? own : 32;
+  const long long blocks = p.prefix_blocks + (long long)p.B * p.Hk * ((G + heads_per - 1) / heads_per) * n_own;
+  // teams of a workgroup that share a head's slices, so that each folds four or fewer of them at a time
+  const int teams = 1024 / D;
+  int by = 1;
+  while (by < teams && by * 4 < p.n_slices) by *= 2;
+  const long long heads = (long long)p.B * p.Hq, merge_blocks = (heads + teams / by - 1) / (teams / by);
+  const int chunks = p.w_out ? (p.T + kFinishRows - 1) / kFinishRows : 0;
+  const long long finish_blocks = merge_blocks + (long long)p.B * p.Hk * chunks;
+  if ((blocks > 0 && !grid_ok(blocks, kShWaves * 64)) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
   if (blocks > 0) {
     auto* kernel = p.prefix_kind == 0 ? slices_kernel<D, 0>(own) : p.prefix_kind == 1 ? slices_kernel<D, 1>(own)
                    : p.prefix_kind == 2 ? slices_kernel<D, 2>(own) : slices_kernel<D, 4>(own);
-    e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kShWaves * 64), stream, p);
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kShWaves * 64), stream, p);
+    if (e != hipSuccess) return e;
   }
-  if (e == hipSuccess) e = launch_kernel(moda_shared_merge_kernel<D>, dim3((unsigned)heads), dim3(D), stream, p);
-  if (e == hipSuccess && weights)
-    e = launch_kernel(moda_shared_weights_kernel, dim3((unsigned)w_blocks), dim3(256), stream, p, chunks);
-  return e;
+  return launch_kernel(moda_shared_finish_kernel<D>, dim3((unsigned)finish_blocks), dim3(256), stream, p, by, (int)merge_blocks, chunks);
 }
 
 hipError_t launch_decode_shared(SharedParams p, int d, void* workspace, hipStream_t stream) {

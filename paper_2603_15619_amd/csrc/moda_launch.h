@@ -87,8 +87,8 @@ struct SharedParams {
   int B, Hq, Hk, T, T_alloc;
   int Np, P, P_alloc;
   int depth_alloc, depth_count;
-  int prefix_kind, prefix_groups, prefix_blocks;  // how prefixes are read, workgroups per prefix, head and column chunk, in all
-  int n_prefix, prefix_per;  // states of a prefix, rows of a slice
+  int prefix_kind, prefix_blocks;  // how prefixes are read, by how many workgroups
+  int n_prefix, prefix_per;  // slices of a prefix, rows of one
   int n_own, own_per;        // slices of an own cache, rows of one
   int n_slices;              // both, and one for the depth slots where there are any
   float scale, scale_log2;
