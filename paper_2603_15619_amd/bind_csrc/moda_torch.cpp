@@ -29,6 +29,12 @@ decltype(&moda_attn_bwd_workspace_bytes) g_bwd_bytes;
 decltype(&moda_attn_decode) g_decode;
 decltype(&moda_attn_decode_workspace_bytes) g_decode_bytes;
 decltype(&moda_depth_append) g_append;
+decltype(&moda_attn_decode_shared) g_shared;
+decltype(&moda_attn_decode_shared_workspace_bytes) g_shared_bytes;
+decltype(&moda_attn_weights) g_weights;
+decltype(&moda_attn_weights_workspace_bytes) g_weights_bytes;
+decltype(&moda_cache_evict) g_evict;
+decltype(&moda_cache_evict_workspace_bytes) g_evict_bytes;
 
 // An argument that must be a plain strided tensor in device memory, or None.
 struct Arg {
@@ -241,18 +247,155 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// (addresses of the six entry points, in the order of the variables above)
-PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  if (nargs != 6) {
-    PyErr_SetString(PyExc_TypeError, "init takes six addresses");
-    return nullptr;
+// The caller's workspace, or a new one of `need()` bytes; false for one that is not plain.
+template <class F>
+bool workspace_arg(const Arg& ws, c10::Device dev, F&& need, at::Tensor& w) {
+  if (!ws.ok || (ws && (!ws->is_contiguous() || ws->device() != dev))) return false;
+  if (ws) {
+    w = *ws.t;
+  } else {
+    const size_t n = need();
+    w = at::empty({(int64_t)(n > 16 ? n : 16)}, at::TensorOptions().dtype(at::kByte).device(dev));
   }
-  void* p[6];
-  for (int i = 0; i < 6; ++i)
+  return true;
+}
+size_t bytes_of(const at::Tensor& w) { return (size_t)w.numel() * w.element_size(); }
+
+// (Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T, depth_count, scale, weights, weights_out,
+//  out, lse, workspace); returns (out, lse)
+PyObject* shared(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(18);
+  const Arg q(a[0]), kp(a[1]), vp(a[2]), k(a[3]), v(a[4]), kd(a[5]), vd(a[6]), plens(a[7]), lens(a[8]), w_in(a[13]), w_out(a[14]),
+      out(a[15]), lse(a[16]), ws(a[17]);
+  for (const Arg* x : {&q, &kp, &vp, &k, &v, &kd, &vd, &plens, &lens, &w_in, &w_out, &out, &lse, &ws})
+    if (!x->ok) Py_RETURN_NONE;
+  if (!g_shared || !q || q->dim() != 3 || !fits(*q.t) || !(k || kp)) Py_RETURN_NONE;
+  if ((kp && (kp->dim() != 4 || !fits(*kp.t))) || (k && (k->dim() != 4 || !fits(*k.t))) || (kd && (kd->dim() != 4 || !fits(*kd.t))))
+    Py_RETURN_NONE;
+  const int64_t B = q->size(0), Hq = q->size(1), d = q->size(2), Hk = (k ? k : kp)->size(1), rows = k ? k->size(2) : 0;
+  const int64_t Np = kp ? kp->size(0) : 1, P_alloc = kp ? kp->size(2) : 0, La = kd ? kd->size(2) : 0;
+  const auto dt = q->scalar_type();
+  const auto dev = q->device();
+  moda_shape s;
+  moda_prefix x;
+  s.B = B; s.Hq = Hq; s.Hk = Hk; s.d = d; s.depth_alloc = La; s.causal = 1;
+  x.n_prefixes = Np; x.prefix_alloc = P_alloc;
+  if (!dtype_code(dt, s.dtype) || !int_arg(a[9], P_alloc, x.prefix_rows) || !int_arg(a[10], rows, s.T) ||
+      !int_arg(a[11], La, s.depth_count) || !scale_arg(a[12], s.scale))
+    Py_RETURN_NONE;
+  if (!q.is(dt, dev, {B, Hq, d}) || !kp.is(dt, dev, {Np, Hk, P_alloc, d}) || !vp.is(dt, dev, {Np, Hk, P_alloc, d}) ||
+      !k.is(dt, dev, {B, Hk, rows, d}) || !v.is(dt, dev, {B, Hk, rows, d}) || !kd.is(dt, dev, {B, Hk, La, d}) ||
+      !vd.is(dt, dev, {B, Hk, La, d}) || !plens.is(at::kInt, dev, {Np}) || !lens.is(at::kInt, dev, {B}) ||
+      !w_in.is(at::kFloat, dev, {B, Hk, rows}) || !w_out.is(at::kFloat, dev, {B, Hk, rows}) || !out.is(dt, dev, {B, Hq, d}) ||
+      !lse.is(at::kFloat, dev, {B, Hq}))
+    Py_RETURN_NONE;
+  at::Tensor w;
+  if (!workspace_arg(ws, dev, [&] { return g_shared_bytes(&x, w_out ? 1 : 0, &s); }, w)) Py_RETURN_NONE;
+  const at::Tensor r[2] = {out ? *out.t : at::empty_like(*q.t), lse ? *lse.t : at::empty({B, Hq}, q->options().dtype(at::kFloat))};
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {q.ptr(), kp.ptr(), vp.ptr(), k.ptr(), v.ptr(), kd.ptr(), vd.ptr(), plens.ptr(), lens.ptr(), w_in.ptr(), w_out.ptr(),
+                     r[0].data_ptr(), r[1].data_ptr(), w.data_ptr()};
+  const size_t ws_bytes = bytes_of(w);
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_shared(p[0], p[1], p[2], p[3], p[4], p[5], p[6], (const int32_t*)p[7], (const int32_t*)p[8], (const float*)p[9],
+                    (float*)p[10], p[11], (float*)p[12], (int32_t)rows, p[13], ws_bytes, &x, &s, st);
+  });
+  return rc == MODA_OK ? tuple_of(r) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// (Q, Kseq, LSE, window, causal, scale, lengths, weights, weights_out, workspace); returns True
+PyObject* weights(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(10);
+  const Arg q(a[0]), k(a[1]), lse(a[2]), lens(a[6]), w_in(a[7]), w_out(a[8]), ws(a[9]);
+  for (const Arg* x : {&q, &k, &lse, &lens, &w_in, &w_out, &ws})
+    if (!x->ok) Py_RETURN_NONE;
+  if (!g_weights || !q || !k || !lse || !w_out || q->dim() != 4 || k->dim() != 4 || !fits(*q.t) || !fits(*k.t)) Py_RETURN_NONE;
+  const int64_t B = q->size(0), Hq = q->size(1), T = q->size(2), d = q->size(3), Hk = k->size(1), rows = k->size(2);
+  const auto dt = q->scalar_type();
+  const auto dev = q->device();
+  moda_shape s;
+  int32_t window;
+  s.B = B; s.Hq = Hq; s.Hk = Hk; s.T = T; s.d = d; s.depth_alloc = 0; s.depth_count = 0;
+  if (a[3] == Py_None || !dtype_code(dt, s.dtype) || !int_arg(a[3], 0, window) || !bool_arg(a[4], s.causal) || !scale_arg(a[5], s.scale))
+    Py_RETURN_NONE;
+  if (!q.is(dt, dev, {B, Hq, T, d}) || !k.is(dt, dev, {B, Hk, rows, d}) || !lse.is(at::kFloat, dev, {B, Hq, T}) ||
+      !lens.is(at::kInt, dev, {B}) || !w_in.is(at::kFloat, dev, {B, Hk, rows}) || !w_out.is(at::kFloat, dev, {B, Hk, rows}))
+    Py_RETURN_NONE;
+  at::Tensor w;
+  if (!workspace_arg(ws, dev, [&] { return g_weights_bytes(window, &s); }, w)) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {q.ptr(), k.ptr(), lse.ptr(), lens.ptr(), w_in.ptr(), w_out.ptr(), w.data_ptr()};
+  const size_t ws_bytes = bytes_of(w);
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_weights(p[0], p[1], (const float*)p[2], (const int32_t*)p[3], (const float*)p[4], (float*)p[5], window, (int32_t)rows, p[6],
+                     ws_bytes, &s, st);
+  });
+  if (rc == MODA_OK) Py_RETURN_TRUE;
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// (Kseq, Vseq, weights, positions, lengths, Kout, Vout, weights_out, positions_out, lengths_out, index, keep, recent, T,
+//  workspace); returns True
+PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(15);
+  const Arg k(a[0]), v(a[1]), w_in(a[2]), pos(a[3]), lens(a[4]), ko(a[5]), vo(a[6]), wo(a[7]), po(a[8]), lo(a[9]), index(a[10]), ws(a[14]);
+  for (const Arg* x : {&k, &v, &w_in, &pos, &lens, &ko, &vo, &wo, &po, &lo, &index, &ws})
+    if (!x->ok) Py_RETURN_NONE;
+  if (!g_evict || !k || !v || !w_in || !ko || !vo || !wo || !lo || !index || k->dim() != 4 || ko->dim() != 4 || !fits(*k.t) || !fits(*ko.t))
+    Py_RETURN_NONE;
+  const int64_t B = k->size(0), Hk = k->size(1), rows = k->size(2), d = k->size(3), out_rows = ko->size(2);
+  const auto dt = k->scalar_type();
+  const auto dev = k->device();
+  moda_shape s;
+  int32_t keep, recent;
+  s.B = B; s.Hq = Hk; s.Hk = Hk; s.d = d; s.depth_alloc = 0; s.depth_count = 0; s.causal = 1; s.scale = 0.f;
+  if (a[11] == Py_None || a[12] == Py_None || a[13] == Py_None || !dtype_code(dt, s.dtype) || !int_arg(a[11], 0, keep) ||
+      !int_arg(a[12], 0, recent) || !int_arg(a[13], 0, s.T))
+    Py_RETURN_NONE;
+  const int64_t n = keep < s.T ? keep : s.T;
+  if (n < 0 || !k.is(dt, dev, {B, Hk, rows, d}) || !v.is(dt, dev, {B, Hk, rows, d}) || !w_in.is(at::kFloat, dev, {B, Hk, rows}) ||
+      !pos.is(at::kInt, dev, {B, Hk, rows}) || !lens.is(at::kInt, dev, {B}) || !ko.is(dt, dev, {B, Hk, out_rows, d}) ||
+      !vo.is(dt, dev, {B, Hk, out_rows, d}) || !wo.is(at::kFloat, dev, {B, Hk, out_rows}) || !po.is(at::kInt, dev, {B, Hk, out_rows}) ||
+      !lo.is(at::kInt, dev, {B}) || !index.is(at::kInt, dev, {B, Hk, n}))
+    Py_RETURN_NONE;
+  at::Tensor w;
+  if (!workspace_arg(ws, dev, [&] { return g_evict_bytes(keep, &s); }, w)) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {k.ptr(), v.ptr(), w_in.ptr(), pos.ptr(), lens.ptr(), ko.ptr(), vo.ptr(), wo.ptr(), po.ptr(), lo.ptr(), index.ptr(),
+                     w.data_ptr()};
+  const size_t ws_bytes = bytes_of(w);
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_evict(p[0], p[1], (const float*)p[2], (const int32_t*)p[3], (const int32_t*)p[4], p[5], p[6], (float*)p[7], (int32_t*)p[8],
+                   (int32_t*)p[9], (int32_t*)p[10], keep, recent, (int32_t)rows, (int32_t)out_rows, p[11], ws_bytes, &s, st);
+  });
+  if (rc == MODA_OK) Py_RETURN_TRUE;
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// n addresses, none of them null; false with the exception set.
+bool addresses(PyObject* const* a, Py_ssize_t nargs, void** p, Py_ssize_t n) {
+  if (nargs != n) {
+    PyErr_Format(PyExc_TypeError, "init takes %zd addresses", n);
+    return false;
+  }
+  for (Py_ssize_t i = 0; i < n; ++i)
     if (!(p[i] = PyLong_AsVoidPtr(a[i]))) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null entry point");
-      return nullptr;
+      return false;
     }
+  return true;
+}
+
+// (addresses of the first six entry points, in the order of the variables above)
+PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  void* p[6];
+  if (!addresses(a, nargs, p, 6)) return nullptr;
   g_bwd = (decltype(g_bwd))p[1];
   g_bwd_bytes = (decltype(g_bwd_bytes))p[2];
   g_decode = (decltype(g_decode))p[3];
@@ -261,9 +404,22 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   g_fwd = (decltype(g_fwd))p[0];
   Py_RETURN_NONE;
 }
+// (... of the six that follow them)
+PyObject* init_cache(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  void* p[6];
+  if (!addresses(a, nargs, p, 6)) return nullptr;
+  g_shared = (decltype(g_shared))p[0];
+  g_shared_bytes = (decltype(g_shared_bytes))p[1];
+  g_weights = (decltype(g_weights))p[2];
+  g_weights_bytes = (decltype(g_weights_bytes))p[3];
+  g_evict = (decltype(g_evict))p[4];
+  g_evict_bytes = (decltype(g_evict_bytes))p[5];
+  Py_RETURN_NONE;
+}
 
 #define MODA_METHOD(f) {#f, (PyCFunction)(void (*)())f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MODA_METHOD(init), MODA_METHOD(fwd), MODA_METHOD(bwd), MODA_METHOD(decode), MODA_METHOD(append),
+                         MODA_METHOD(init_cache), MODA_METHOD(shared), MODA_METHOD(weights), MODA_METHOD(evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "moda_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

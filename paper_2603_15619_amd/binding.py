@@ -4,8 +4,8 @@ Argument marshalling only: torch tensors supply device memory and the stream;
 every step of the attention runs in the HIP kernels of libmoda.so.  There is no
 fallback: if the library is missing or a call is rejected, an exception is raised.
 
-Plain valid calls of moda_attn_fwd, moda_attn_bwd, moda_attn_decode and moda_depth_append are marshalled
-by moda_torch.so (bind_csrc/moda_torch.cpp); whatever it declines comes back as None and is taken here,
+Plain valid calls of moda_attn_fwd, moda_attn_bwd, moda_attn_decode, moda_depth_append and of the calls on a shared or
+bounded cache are marshalled by moda_torch.so (bind_csrc/moda_torch.cpp); whatever it declines comes back as None and is taken here,
 through ctypes, with the same checks and an exception for the one that fails.
 """
 import ctypes
@@ -136,6 +136,9 @@ def _native():
         m.init(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                  (L.moda_attn_fwd, L.moda_attn_bwd, L.moda_attn_bwd_workspace_bytes, L.moda_attn_decode,
                   L.moda_attn_decode_workspace_bytes, L.moda_depth_append)))
+        m.init_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                       (L.moda_attn_decode_shared, L.moda_attn_decode_shared_workspace_bytes, L.moda_attn_weights,
+                        L.moda_attn_weights_workspace_bytes, L.moda_cache_evict, L.moda_cache_evict_workspace_bytes)))
         _native_module = m
     return _native_module
 
@@ -350,6 +353,10 @@ def _workspace(workspace, need, device):
 
 def _decode_shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T, depth_count, scale,
                    weights, weights_out, out, lse, workspace):
+    r = (_native_module or _native()).shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T,
+                                             depth_count, scale, weights, weights_out, out, lse, workspace)
+    if r is not None:
+        return _outputs(r)
     B, Hq, d = Q.shape
     if Kseq is None and Kprefix is None:
         raise ValueError("Kseq or Kprefix must be given")
@@ -425,6 +432,12 @@ def moda_attn_weights(Q, Kseq, LSE, window=0, causal=True, scale=None, lengths=N
     Q [B,Hq,T,d] (T <= kv_alloc) whose log-sum-exp LSE [B,Hq,T] the forward pass left, summed over queries and the heads of
     a group; of the last `window` queries only unless that is 0.  lengths [B] (int32): the filled positions of each
     sequence.  Added to `weights` where given, in place unless weights_out is."""
+    if weights_out is None:
+        weights_out = weights if weights is not None else torch.zeros(Kseq.shape[:3], dtype=torch.float32, device=Q.device)
+    r = (_native_module or _native()).weights(Q, Kseq, LSE, window, causal, scale, lengths, weights, weights_out, workspace)
+    if r is not None:
+        _outputs(r)
+        return weights_out
     B, Hq, T, d = Q.shape
     Hk, kv_alloc = Kseq.shape[1], Kseq.shape[2]
     dev, dt = Q.device, Q.dtype
@@ -432,8 +445,6 @@ def moda_attn_weights(Q, Kseq, LSE, window=0, causal=True, scale=None, lengths=N
     _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
     _require(LSE, "LSE", (B, Hq, T), torch.float32, dev)
     _require(lengths, "lengths", (B,), torch.int32, dev)
-    if weights_out is None:
-        weights_out = weights if weights is not None else torch.zeros((B, Hk, kv_alloc), dtype=torch.float32, device=dev)
     _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
     _require(weights_out, "weights_out", (B, Hk, kv_alloc), torch.float32, dev)
     s = MODAShape(B, Hq, Hk, T, d, 0, 0, int(bool(causal)), float(scale) if scale else 0.0, _dtype_code(Q))
@@ -461,6 +472,15 @@ def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, length
     if Kout.dim() != 4:
         raise ValueError("Kout: expected a [B,Hk,out_alloc,d] tensor")
     out_alloc = Kout.shape[2]
+    if lengths_out is None:
+        lengths_out = lengths if lengths is not None and out is None else torch.empty(B, dtype=torch.int32, device=dev)
+    if index is None:
+        index = torch.empty((B, Hk, n), dtype=torch.int32, device=dev)
+    r = (_native_module or _native()).evict(Kseq, Vseq, weights, positions, lengths, Kout, Vout, W_out, P_out, lengths_out, index,
+                                            keep, recent, T, workspace)
+    if r is not None:
+        _outputs(r)
+        return index, lengths_out
     _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
     _require(Vseq, "Vseq", (B, Hk, kv_alloc, d), dt, dev)
     _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
@@ -470,10 +490,6 @@ def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, length
     _require(Vout, "Vout", (B, Hk, out_alloc, d), dt, dev)
     _require(W_out, "weights_out", (B, Hk, out_alloc), torch.float32, dev)
     _require(P_out, "positions_out", (B, Hk, out_alloc), torch.int32, dev)
-    if lengths_out is None:
-        lengths_out = lengths if lengths is not None and out is None else torch.empty(B, dtype=torch.int32, device=dev)
-    if index is None:
-        index = torch.empty((B, Hk, n), dtype=torch.int32, device=dev)
     _require(lengths_out, "lengths_out", (B,), torch.int32, dev)
     _require(index, "index", (B, Hk, n), torch.int32, dev)
     s = MODAShape(B, Hk, Hk, T, d, 0, 0, 1, 0.0, _dtype_code(Kseq))
