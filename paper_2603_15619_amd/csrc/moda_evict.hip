@@ -20,15 +20,25 @@ __device__ __forceinline__ unsigned weight_key(float w) {
   return w != w ? 0u : u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
+// Workspace of the long caches: bits and list of every (sequence, head).
+struct EvictScratch {
+  unsigned long long* bits;
+  size_t words;  // of one
+  int* list;
+};
+
 // Rows of a (sequence, head): wave w takes `steps` times 64 of them, from w * steps * 64 on.  N > 0: steps = N, and a row's key stays in
 // a register from its one read on; 0: as many steps as it takes, and every pass reads weights and positions again.
 template <int N>
-__global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictParams p, int* movers_ws) {
+__global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictParams p, EvictScratch ws) {
   constexpr int kBins = 2048;
   __shared__ unsigned hist[kBins];
   __shared__ int part[kEvWaves], part2[kEvWaves];
   __shared__ unsigned s_digit;
   __shared__ int s_need;
+  // rows that stay, a bit each; rows that move, in ascending order (half of all at most: as many as there are holes)
+  __shared__ unsigned long long lds_bits[N > 0 ? kEvWaves * N : 1];
+  __shared__ unsigned short lds_list[N > 0 ? kEvThreads * N / 2 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bg = blockIdx.x, b = bg / p.Hk;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
@@ -43,6 +53,8 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   const int* pos = p.positions ? p.positions + (size_t)bg * p.T_alloc : nullptr;
   const int steps = N > 0 ? N : (len + kEvThreads - 1) / kEvThreads;
   const int r0 = wave * steps * 64 + lane;  // the lane's rows: r0 + 64 i
+  auto* bits = [&] { if constexpr (N > 0) return lds_bits; else return ws.bits + (size_t)bg * ws.words; }();
+  auto* list = [&] { if constexpr (N > 0) return lds_list; else return ws.list + (size_t)bg * p.n; }();
   unsigned keys[N > 0 ? N : 1];
   // N > 0: bounds-checked loads from one address register; rows past the end read as 0
   const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc((void*)w, 0, N > 0 ? len * 4 : 0, 0x00020000);
@@ -150,41 +162,47 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   __syncthreads();
   const int ties_before = before(part);
   __syncthreads();
-  auto walk = [&](auto&& f) {  // f(row, stays) for every row, in order, all lanes
-    int seen = ties_before;
-    each([&](int i) {
-      const int r = r0 + i * 64;
-      const unsigned k = key_of(i);
-      const unsigned long long tie = __ballot(r < len && k == threshold);
-      const bool is_tie = (tie >> lane) & 1;
-      f(r, r < len && (is_tie ? seen + __popcll(tie & below) < need : k > threshold));
-      seen += __popcll(tie);
-    });
-  };
-  int holes = 0, movers = 0;
-  walk([&](int r, bool stays) {
-    holes += __popcll(__ballot(r < fit && !stays));
-    movers += __popcll(__ballot(r >= fit && stays));
+  // which rows stay, one word of bits per step (`bits`), and the waves' holes below the new length and rows to move behind it
+  int seen = ties_before, holes = 0, movers = 0;
+  each([&](int i) {
+    const int r = r0 + i * 64, base = r - lane;
+    const unsigned k = key_of(i);
+    const unsigned long long tie = __ballot(r < len && k == threshold);
+    unsigned long long stay = __ballot(r < len && k > threshold);
+    if (seen + __popcll(tie) <= need) stay |= tie;
+    else stay |= __ballot(((tie >> lane) & 1) && seen + __popcll(tie & below) < need);
+    seen += __popcll(tie);
+    if (lane == 0) bits[wave * steps + i] = stay;
+    const unsigned long long low = fit - base >= 64 ? ~0ull : fit <= base ? 0ull : (1ull << (fit - base)) - 1;
+    holes += __popcll(low & ~stay);
+    movers += __popcll(stay & ~low);
   });
   if (lane == 0) {
     part[wave] = holes;
     part2[wave] = movers;
   }
   __syncthreads();
-  int* list = movers_ws + (size_t)bg * p.n;
   int nth = before(part2);
-  walk([&](int r, bool stays) {
-    const unsigned long long mv = __ballot(r >= fit && stays);
+#pragma unroll 4
+  for (int i = 0; i < steps; ++i) {
+    const int r = r0 + i * 64, base = r - lane;
+    if (base + 64 <= fit) continue;  // (uniform)
+    const unsigned long long stay = bits[wave * steps + i];
+    const unsigned long long mv = fit <= base ? stay : stay & ~((1ull << (fit - base)) - 1);
     if ((mv >> lane) & 1) list[nth + __popcll(mv & below)] = r;
     nth += __popcll(mv);
-  });
+  }
   __syncthreads();
   nth = before(part);
-  walk([&](int r, bool stays) {
-    const unsigned long long ho = __ballot(r < fit && !stays);
-    if (r < fit) index[r] = stays ? r : list[nth + __popcll(ho & below)];
-    nth += __popcll(ho);
-  });
+#pragma unroll 4
+  for (int i = 0; i < steps; ++i) {
+    const int r = r0 + i * 64, base = r - lane;
+    if (base >= fit) continue;  // (uniform)
+    const unsigned long long stay = bits[wave * steps + i], low = fit - base >= 64 ? ~0ull : (1ull << (fit - base)) - 1;
+    const unsigned long long hole = low & ~stay;
+    if (r < fit) index[r] = ((hole >> lane) & 1) ? list[nth + __popcll(hole & below)] : r;
+    nth += __popcll(hole);
+  }
 }
 
 // 16 bytes of K and of V per thread; the thread of a row's first 16 bytes moves its weight and position.
@@ -207,8 +225,13 @@ __global__ __launch_bounds__(256) void moda_evict_move_kernel(EvictParams p, int
   }
 }
 
+// Longest cache whose keys stay in registers.
+constexpr int kEvInRegisters = 32 * kEvThreads;
+static size_t bit_words(int T) { return (size_t)((T + kEvThreads - 1) / kEvThreads) * kEvWaves; }
+
 size_t evict_workspace_bytes(int B, int Hk, int T, int keep) {
-  return std::max<size_t>(16, (size_t)B * Hk * std::min(keep, T) * sizeof(int));
+  if (T <= kEvInRegisters) return 16;
+  return (size_t)B * Hk * (bit_words(T) * sizeof(unsigned long long) + std::min(keep, T) * sizeof(int));
 }
 
 hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t stream) {
@@ -216,11 +239,17 @@ hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t strea
   const int per_row = p.row_bytes / 16;
   const long long chunks = ((long long)p.n * per_row + 255) / 256;
   if (!grid_ok(groups, kEvThreads) || chunks > 0x7fffffff || !grid_ok(groups * chunks, 256)) return kGridTooLarge;
+  EvictScratch ws = {};
+  if (p.T > kEvInRegisters) {
+    ws.words = bit_words(p.T);
+    ws.bits = (unsigned long long*)workspace;
+    ws.list = (int*)(ws.bits + (size_t)groups * ws.words);
+  }
   auto* choose = p.T <= 1 * kEvThreads ? moda_evict_choose_kernel<1> : p.T <= 2 * kEvThreads ? moda_evict_choose_kernel<2>
                  : p.T <= 4 * kEvThreads ? moda_evict_choose_kernel<4> : p.T <= 8 * kEvThreads ? moda_evict_choose_kernel<8>
-                 : p.T <= 16 * kEvThreads ? moda_evict_choose_kernel<16> : p.T <= 32 * kEvThreads ? moda_evict_choose_kernel<32>
+                 : p.T <= 16 * kEvThreads ? moda_evict_choose_kernel<16> : p.T <= kEvInRegisters ? moda_evict_choose_kernel<32>
                  : moda_evict_choose_kernel<0>;
-  const hipError_t e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p, (int*)workspace);
+  const hipError_t e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p, ws);
   if (e != hipSuccess) return e;
   return launch_kernel(moda_evict_move_kernel, dim3((unsigned)(groups * chunks)), dim3(256), stream, p, per_row, (int)chunks);
 }
