@@ -205,24 +205,42 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   }
 }
 
-// 16 bytes of K and of V per thread; the thread of a row's first 16 bytes moves its weight and position.
-__global__ __launch_bounds__(256) void moda_evict_move_kernel(EvictParams p, int per_row, int n_chunks) {
+// Two 16-byte pieces of K and of V per thread, all loaded before any store; the thread of a row's first piece moves its weight and
+// position.
+constexpr int kMovePieces = 2;
+__global__ __launch_bounds__(256) void moda_evict_move_kernel(EvictParams p, int per_row_log2, int n_chunks) {
   const int bg = blockIdx.x / n_chunks, b = bg / p.Hk;
-  const long long i = (long long)(blockIdx.x % n_chunks) * 256 + threadIdx.x;
-  const int r = (int)(i / per_row), c = (int)(i % per_row);
-  if (p.lengths_out && i == 0 && bg == b * p.Hk)
+  const long long i0 = (long long)(blockIdx.x % n_chunks) * (256 * kMovePieces) + threadIdx.x;
+  if (p.lengths_out && i0 == 0 && bg == b * p.Hk)
     p.lengths_out[b] = min(p.keep, p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T);
-  if (r >= p.n) return;
-  const int src = p.index[(size_t)bg * p.n + r];
-  if (src < 0 || (p.in_place && src == r)) return;
-  const size_t from = (size_t)bg * p.T_alloc + src, to = (size_t)bg * p.out_alloc + r;
-  const u32x4 k = *(const u32x4*)(p.K + from * p.row_bytes + c * 16), v = *(const u32x4*)(p.V + from * p.row_bytes + c * 16);
-  *(u32x4*)(p.K_out + to * p.row_bytes + c * 16) = k;
-  *(u32x4*)(p.V_out + to * p.row_bytes + c * 16) = v;
-  if (c == 0) {
-    p.w_out[to] = p.w[from];
-    if (p.positions) p.positions_out[to] = p.positions[from];
+  u32x4 k[kMovePieces], v[kMovePieces];
+  long long from[kMovePieces], to[kMovePieces];  // rows; from < 0: nothing to move
+  const int c = (int)(i0 & ((1 << per_row_log2) - 1));
+#pragma unroll
+  for (int u = 0; u < kMovePieces; ++u) {
+    const long long r = (i0 + u * 256) >> per_row_log2;
+    int src = -1;
+    if (r < p.n) src = p.index[(size_t)bg * p.n + r];
+    if (p.in_place && src == r) src = -1;
+    from[u] = src < 0 ? -1 : (long long)bg * p.T_alloc + src;
+    to[u] = (long long)bg * p.out_alloc + r;
   }
+#pragma unroll
+  for (int u = 0; u < kMovePieces; ++u)
+    if (from[u] >= 0) {
+      k[u] = __builtin_nontemporal_load((const u32x4*)(p.K + from[u] * p.row_bytes) + c);
+      v[u] = __builtin_nontemporal_load((const u32x4*)(p.V + from[u] * p.row_bytes) + c);
+    }
+#pragma unroll
+  for (int u = 0; u < kMovePieces; ++u)
+    if (from[u] >= 0) {
+      __builtin_nontemporal_store(k[u], (u32x4*)(p.K_out + to[u] * p.row_bytes) + c);
+      __builtin_nontemporal_store(v[u], (u32x4*)(p.V_out + to[u] * p.row_bytes) + c);
+      if (c == 0) {
+        p.w_out[to[u]] = p.w[from[u]];
+        if (p.positions) p.positions_out[to[u]] = p.positions[from[u]];
+      }
+    }
 }
 
 // Longest cache whose keys stay in registers.
@@ -236,8 +254,8 @@ size_t evict_workspace_bytes(int B, int Hk, int T, int keep) {
 
 hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t stream) {
   const long long groups = (long long)p.B * p.Hk;
-  const int per_row = p.row_bytes / 16;
-  const long long chunks = ((long long)p.n * per_row + 255) / 256;
+  const int per_row_log2 = p.row_bytes == 128 ? 3 : p.row_bytes == 256 ? 4 : 5;  // pieces of 16 bytes of a row: 8, 16 or 32
+  const long long chunks = (((long long)p.n << per_row_log2) + 256 * kMovePieces - 1) / (256 * kMovePieces);
   if (!grid_ok(groups, kEvThreads) || chunks > 0x7fffffff || !grid_ok(groups * chunks, 256)) return kGridTooLarge;
   EvictScratch ws = {};
   if (p.T > kEvInRegisters) {
@@ -251,7 +269,7 @@ hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t strea
                  : moda_evict_choose_kernel<0>;
   const hipError_t e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p, ws);
   if (e != hipSuccess) return e;
-  return launch_kernel(moda_evict_move_kernel, dim3((unsigned)(groups * chunks)), dim3(256), stream, p, per_row, (int)chunks);
+  return launch_kernel(moda_evict_move_kernel, dim3((unsigned)(groups * chunks)), dim3(256), stream, p, per_row_log2, (int)chunks);
 }
 
 }  // namespace moda
