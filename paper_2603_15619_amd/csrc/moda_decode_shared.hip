@@ -23,8 +23,31 @@ namespace moda {
 
 constexpr int kShWaves = 4;
 
-// Floats of a slice's state of one head: channels, reference, normaliser, two unused (so that states are aligned).
-constexpr int state_floats(int d) { return d + 4; }
+// The states in the workspace: O, [state][d], and (reference, normaliser), [state][2].  A slice's states of all its heads are
+// adjacent, so that a workgroup writes whole cache lines: prefixes [n_prefixes, Hk, slice, sequence, head of the group], behind
+// them own rows [B, Hk, slice, head of the group].
+struct HeadStates {  // of one (sequence, query head): prefix slices at first + s * step, the others at own + s * own_step
+  size_t first, own;
+  int step, own_step;
+  __device__ __forceinline__ HeadStates(const SharedParams& p, int b, int g, int j) {
+    const int per = p.B / p.Np, G = p.Hq / p.Hk;
+    step = per * G;
+    own_step = G;
+    first = ((size_t)(b / per * p.Hk + g) * p.n_prefix) * step + b % per * G + j;
+    own = (size_t)p.B * p.Hq * p.n_prefix + ((size_t)(b * p.Hk + g) * p.n_own) * G + j;
+  }
+  __device__ __forceinline__ size_t operator()(const SharedParams& p, int s) const {
+    return s < p.n_prefix ? first + (size_t)s * step : own + (size_t)(s - p.n_prefix) * own_step;
+  }
+};
+
+// Rows of K and V: n of one run, then n2 of another (a slice of an own cache, then the slots).
+struct Rows {
+  const char *K, *V;
+  int n;
+  const char *K2, *V2;
+  int n2;
+};
 
 __device__ __forceinline__ int filled(const int* lengths, int i, int most) {
   return lengths ? min(max(lengths[i], 0), most) : most;
@@ -33,10 +56,10 @@ __device__ __forceinline__ int filled(const int* lengths, int i, int most) {
 // ---------------------------------------------------------------- rows on the vector ALUs
 // A lane owns 8 channels, d/8 lanes a row; a wave takes kU batches of 64 / (d/8) rows at a time, the next ones in
 // flight, and raises its reference once for them.  `q` = GT query rows (heads from nh on repeat the last one and are not
-// stored), `dst` = the first head's state of this slice, `scores` = the first head's logits of these rows, or null.
+// stored), `o_out`, `ml_out` = the first head's state, `scores` = the first head's logits of the first run, or null.
 template <int D, int GT>
-__device__ __forceinline__ void read_rows(const char* K, const char* V, int n, const char* q_rows, int nh, float c2, float* dst,
-                                          size_t dst_step, float* scores, size_t score_step, float* red) {
+__device__ __forceinline__ void read_rows(const Rows& x, const char* q_rows, int nh, float c2, float* o_out,
+                                          float* ml_out, float* scores, size_t score_step, float* red) {
   constexpr int LPR = D / 8, RPS = 64 / LPR, RB = D * 2, kU = 4, STEP = kShWaves * kU * RPS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = lane / LPR, l16 = lane % LPR;
   u32x4 q[GT];
@@ -49,16 +72,18 @@ __device__ __forceinline__ void read_rows(const char* K, const char* V, int n, c
 #pragma unroll
     for (int k = 0; k < 8; ++k) o[j][k] = 0.f;
   }
-  const int row0 = wave * kU * RPS + rg;
+  const int row0 = wave * kU * RPS + rg, n = x.n + x.n2;
   if (n > 0) {  // (uniform)
-    auto load = [&](const char* base, int r) {
-      return __builtin_nontemporal_load((const u32x4*)(base + (size_t)min(r, n - 1) * RB + l16 * 16));
+    auto load = [&](const char* first, const char* second, int r) {
+      r = min(r, n - 1);
+      const char* at = r < x.n ? first + (size_t)r * RB : second + (size_t)(r - x.n) * RB;
+      return __builtin_nontemporal_load((const u32x4*)(at + l16 * 16));
     };
     u32x4 kn[kU], vn[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      kn[u] = load(K, row0 + u * RPS);
-      vn[u] = load(V, row0 + u * RPS);
+      kn[u] = load(x.K, x.K2, row0 + u * RPS);
+      vn[u] = load(x.V, x.V2, row0 + u * RPS);
     }
     for (int base = 0; base < n; base += STEP) {  // (uniform)
       const int r = row0 + base;
@@ -71,8 +96,8 @@ __device__ __forceinline__ void read_rows(const char* K, const char* V, int n, c
       if (base + STEP < n) {  // (uniform)
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-          kn[u] = load(K, r + STEP + u * RPS);
-          vn[u] = load(V, r + STEP + u * RPS);
+          kn[u] = load(x.K, x.K2, r + STEP + u * RPS);
+          vn[u] = load(x.V, x.V2, r + STEP + u * RPS);
         }
       } else {  // rows past the end repeat the last one with weight zero, which an infinite value would turn into NaN
 #pragma unroll
@@ -94,7 +119,7 @@ __device__ __forceinline__ void read_rows(const char* K, const char* V, int n, c
 #pragma unroll
           for (int u = 1; u < kU; ++u) a = l16 == u ? sc[u] : a;
           const int at = r + l16 * RPS;
-          if (l16 < kU && at < n && j < nh) scores[(size_t)j * score_step + at] = a;
+          if (l16 < kU && at < x.n && j < nh) scores[(size_t)j * score_step + at] = a;
         }
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
@@ -137,12 +162,8 @@ __device__ __forceinline__ void read_rows(const char* K, const char* V, int n, c
       ll += f * x[D + 1];
       oo += f * x[ch];
     }
-    float* to = dst + j * dst_step;
-    to[ch] = oo;
-    if (ch == 0) {
-      to[D] = mm;
-      to[D + 1] = ll;
-    }
+    o_out[j * D + ch] = oo;
+    if (ch == 0) *(f32x2*)(ml_out + j * 2) = (f32x2){mm, ll};
   }
 }
 
@@ -165,9 +186,11 @@ struct Columns {
     l = 0.f;
   }
   // NB blocks of 32 rows: K rows from LDS address `k`, V rows from `v` (layout of Tile<D>); `left` = rows that count.
-  // The logits of the lane's column (before the scale) go to scores[row], if not null.
+  // `scores` (a block of 32 rows only), if not null: column q's logits, before the scale, go to scores[q * step + row], q < n.
   template <int NB>
-  __device__ __forceinline__ void fold(unsigned k, unsigned v, const FragAddr<D>& fa, int hi, int left, float c2, float* scores) {
+  __device__ __forceinline__ void fold(unsigned k, unsigned v, const FragAddr<D>& fa, int lane, int left, float c2, float* scores = nullptr,
+                                       size_t step = 0, int n = 0) {
+    const int hi = lane >> 5;
     f32x16 s[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -179,20 +202,27 @@ struct Columns {
 #pragma unroll
       for (int b = 0; b < NB; ++b) s[b] = mfma_bf16(FragAddr<D>::row_frag(xk, b, 0), q[st], s[b]);
     }
-    if (scores) {
+    if (NB == 1 && scores) {  // (uniform)
+      // through the K tile, which has been read: 8 pieces of four rows per column, of which eight lanes store a whole cache line
+      // (16 x 3100 rows, 64 heads on 8, d = 64: whole call 33.1 us, 33.7 with 16-byte stores from where the logits are)
+      const int l32 = lane & 31;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int i = 0; i < 4; ++i)
+        if (l32 < n)
+          *(f32x4 __attribute__((address_space(3)))*)(size_t)(k + l32 * 128 + (((i * 2 + hi) ^ (l32 & 7)) << 4)) =
+              (f32x4){s[0][4 * i], s[0][4 * i + 1], s[0][4 * i + 2], s[0][4 * i + 3]};
+      for (int q = lane >> 3; q < n; q += 8) {
+        const int row = (lane & 7) * 4;
+        const f32x4 x = *(const f32x4 __attribute__((address_space(3)))*)(size_t)(k + q * 128 + (((lane & 7) ^ (q & 7)) << 4));
+        float* to = scores + q * step + row;
+        if (row + 4 <= left) {
+          *(f32x4*)to = x;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = b * 32 + i * 8 + hi * 4;
-          if (row + 4 <= left) {
-            *(f32x4*)(scores + row) = (f32x4){s[b][4 * i], s[b][4 * i + 1], s[b][4 * i + 2], s[b][4 * i + 3]};
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (row + j < left) scores[row + j] = s[b][4 * i + j];
-          }
+          for (int j = 0; j < 4; ++j)
+            if (row + j < left) to[j] = x[j];
         }
+      }
     }
     if (left < NB * 32) {  // (uniform)
 #pragma unroll
@@ -244,12 +274,12 @@ struct Columns {
   }
 };
 
-// The states of a workgroup's waves, those with the same columns (wave % CW) folded, to column -> dst(column) (null: a column
-// past the last query).  LDS: a wave's O^T as 16-byte pieces of four channels, piece c of column q at 32 c + (q ^ c % 32) of
+// The states of a workgroup's waves, those with the same columns (wave % CW) folded, to the first n of CW * 32 adjacent states.  LDS: a wave's O^T as 16-byte pieces of four channels, piece c of column q at 32 c + (q ^ c % 32) of
 // the wave's part, so that both the writes (32 columns of a piece) and the reads (the pieces of a column, which make
 // whole rows in memory) touch every bank alike.
-template <int D, int CW, class Dst>
-__device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* smem, float (*stat)[32][2], float c2, Dst&& dst) {
+template <int D, int CW>
+__device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* smem, float (*stat)[32][2], float c2, int n, float* o_out,
+                                           float* ml_out) {
   constexpr int KW = kShWaves / CW, kPieces = D / 4, kPart = 32 * D * 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hi = lane >> 5;
   const float l_all = pair_sum(c.l);
@@ -270,8 +300,7 @@ __device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* s
 #pragma unroll
   for (int i = tid; i < CW * 32 * kPieces; i += kShWaves * 64) {
     const int col = i / kPieces, piece = i % kPieces, cw = col / 32, q = col % 32;
-    float* to = dst(col);
-    if (!to) continue;
+    if (col >= n) continue;
     float m = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -286,23 +315,22 @@ __device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* s
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += f * x[j];
     }
-    *(f32x4*)(to + piece * 4) = o;
-    if (piece == 0) *(f32x2*)(to + D) = (f32x2){m, l};
+    *(f32x4*)(o_out + col * D + piece * 4) = o;
+    if (piece == 0) *(f32x2*)(ml_out + col * 2) = (f32x2){m, l};
   }
 }
 
-// Every wave by itself: n rows at K and V (its part of the slice), 32 at a time through its two LDS tiles at `lds`; the next
-// block(s) are in flight in registers.  Rows past the end read as zeros (bounds-checked buffers) and fetch nothing.
-constexpr int waves_ahead(int d) { return d == 64 ? 2 : 1; }  // (d = 128: registers for one)
-template <int D>
-__device__ __forceinline__ void read_by_wave(Columns<D>& c, const char* K, const char* V, int n, unsigned lds, float c2, float* scores) {
+// Every wave by itself: the rows x, 32 at a time through its two LDS tiles at `lds`; the next block(s) are in flight in
+// registers.  Rows past the end of a run read as zeros (bounds-checked buffers) and fetch nothing.
+template <int D, int kPF>
+__device__ __forceinline__ void read_by_wave(Columns<D>& c, const Rows& x, unsigned lds, float c2, float* scores = nullptr, size_t step = 0,
+                                             int nh = 0) {
   using Tl = Tile<D>;
-  constexpr int RB = D * 2, kInst = 32 * RB / 1024, kHalf = 32 * RB, kPF = waves_ahead(D);
-  const int lane = threadIdx.x & 63, hi = lane >> 5;
+  constexpr int RB = D * 2, kInst = 32 * RB / 1024, kHalf = 32 * RB;
+  const int lane = threadIdx.x & 63;
   FragAddr<D> fa;
   fa.init(lane);
-  const __amdgpu_buffer_rsrc_t k_buf = __builtin_amdgcn_make_buffer_rsrc((void*)K, 0, n * RB, 0x00020000);
-  const __amdgpu_buffer_rsrc_t v_buf = __builtin_amdgcn_make_buffer_rsrc((void*)V, 0, n * RB, 0x00020000);
+  const int n1 = (x.n + 31) / 32, n_blocks = n1 + (x.n2 + 31) / 32;
   const int jr = lane / Tl::kChunks, pc = lane % Tl::kChunks;
   const int g_off = jr * RB + ((pc ^ Tl::swz(jr)) << 4);
   auto piece_xor = [](int q) { return (D == 128 ? (q & 3) : ((q & 1) << 1)) << 4; };
@@ -310,7 +338,10 @@ __device__ __forceinline__ void read_by_wave(Columns<D>& c, const char* K, const
     u32x4 k[kInst], v[kInst];
   };
   auto issue = [&](int blk, Block& r) {
-    const int soff = blk * kHalf;
+    const bool first = blk < n1;  // (uniform)
+    const int size = (first ? x.n : x.n2) * RB, soff = (first ? blk : blk - n1) * kHalf;
+    const __amdgpu_buffer_rsrc_t k_buf = __builtin_amdgcn_make_buffer_rsrc((void*)(first ? x.K : x.K2), 0, size, 0x00020000);
+    const __amdgpu_buffer_rsrc_t v_buf = __builtin_amdgcn_make_buffer_rsrc((void*)(first ? x.V : x.V2), 0, size, 0x00020000);
 #pragma unroll
     for (int q = 0; q < kInst; ++q)
       r.k[q] = __builtin_amdgcn_raw_buffer_load_b128(k_buf, xor_here(g_off, piece_xor(q)), soff + q * 1024, 2);
@@ -318,7 +349,6 @@ __device__ __forceinline__ void read_by_wave(Columns<D>& c, const char* K, const
     for (int q = 0; q < kInst; ++q)
       r.v[q] = __builtin_amdgcn_raw_buffer_load_b128(v_buf, xor_here(g_off, piece_xor(q)), soff + q * 1024, 2);
   };
-  const int n_blocks = (n + 31) / 32;
   Block buf[kPF];
 #pragma unroll
   for (int i = 0; i < kPF; ++i) issue(i, buf[i]);
@@ -334,44 +364,64 @@ __device__ __forceinline__ void read_by_wave(Columns<D>& c, const char* K, const
       for (int q = 0; q < kInst; ++q)
         *(u32x4 __attribute__((address_space(3)))*)(size_t)(lds + kHalf + q * 1024 + lane * 16) = buf[i].v[q];
       issue(blk + kPF, buf[i]);
-      if (blk < n_blocks) c.template fold<1>(lds, lds + kHalf, fa, hi, n - blk * 32, c2, scores ? scores + blk * 32 : nullptr);
+      if (blk < n_blocks)
+        c.template fold<1>(lds, lds + kHalf, fa, lane, blk < n1 ? x.n - blk * 32 : x.n2 - (blk - n1) * 32, c2,
+                           scores && blk < n1 ? scores + blk * 32 : nullptr, step, nh);
     }
   }
 }
 
-// The workgroup together: KW x 32 (or 64, KW = 1) rows at a time in a ring of two stages; a wave folds all of them (KW = 1) or its
-// 32 of them (KW = 2: waves 2 and 3 hold the columns of waves 0 and 1).
+// The workgroup together: tiles of kRows rows in a ring of kStages stages, all but one of them in flight while one is folded; a wave
+// folds all rows of a tile (KW = 1) or 32 of its 64 (KW = 2: waves 2 and 3 hold the columns of waves 0 and 1).
+constexpr int ring_bytes(int d) { return d * 512; }
+template <int D, int KW>
+struct Ring {
+  static constexpr int kRows = D == 128 && KW == 1 ? 32 : 64;
+  static constexpr int kTile = kRows * D * 2, kStages = ring_bytes(D) / (2 * kTile);
+};
 template <int D, int KW>
 __device__ __forceinline__ void read_by_workgroup(Columns<D>& c, bool idle, const char* K, const char* V, int n, unsigned lds, float c2) {
   using Tl = Tile<D>;
-  constexpr int RB = D * 2, kStage = 2 * Tl::kBytes;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5;
+  using R = Ring<D, KW>;
+  constexpr int RB = D * 2, kInst = R::kTile / 1024 / kShWaves;  // copies of 1 KB of a wave, of K and of V
+  static_assert(kInst == 2 || kInst == 4, "piece_xor(wave * kInst + i) = piece_xor(wave * kInst) ^ piece_xor(i)");
+  using Loader = TileLoader<D, kShWaves>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   FragAddr<D> fa;
   fa.init(lane);
-  TileLoader<D, kShWaves> loader;
-  loader.init(wave, lane);
+  const int j = lane / Tl::kChunks;
+  const int g_off = (j * RB + (((lane % Tl::kChunks) ^ Tl::swz(j)) << 4)) ^ Loader::piece_xor(wave * kInst);
   const i32x4 k_buf = make_tile_buffer(K, (unsigned)n * RB), v_buf = make_tile_buffer(V, (unsigned)n * RB);
-  auto issue = [&](int i) {
-    const unsigned at = lds + (i & 1) * kStage;
-    loader.issue(k_buf, i * 64, at);
-    loader.issue(v_buf, i * 64, at + Tl::kBytes);
+  // (tiles past the end are asked for as well: they fetch nothing, and the number of copies in flight stays the same)
+  auto issue = [&](int i, int stage) {
+    const unsigned at = lds + stage * 2 * R::kTile + wave * kInst * 1024;
+#pragma unroll
+    for (int q = 0; q < kInst; ++q)
+      tile_copy16(k_buf, xor_here(g_off, Loader::piece_xor(q)), i * R::kTile + (wave * kInst + q) * 1024, at + q * 1024);
+#pragma unroll
+    for (int q = 0; q < kInst; ++q)
+      tile_copy16(v_buf, xor_here(g_off, Loader::piece_xor(q)), i * R::kTile + (wave * kInst + q) * 1024, at + R::kTile + q * 1024);
   };
-  const int n_tiles = (n + 63) / 64;
-  if (n_tiles > 0) issue(0);
+  const int n_tiles = (n + R::kRows - 1) / R::kRows;
+#pragma unroll
+  for (int i = 0; i < R::kStages - 1; ++i) issue(i, i);
+  int stage = 0;
   for (int i = 0; i < n_tiles; ++i) {
-    wait_copies();
-    __syncthreads();  // the tile is there, and everybody is done with the other stage
-    if (i + 1 < n_tiles) issue(i + 1);
-    const unsigned k = lds + (i & 1) * kStage;
-    const int left = n - i * 64;
+    wait_own_copies<(R::kStages - 2) * 2 * kInst>();
+    __syncthreads();  // the tile is there, and everybody is done with the one before it, whose stage is free
+    issue(i + R::kStages - 1, stage == 0 ? R::kStages - 1 : stage - 1);
+    const unsigned k = lds + stage * 2 * R::kTile;
+    stage = stage == R::kStages - 1 ? 0 : stage + 1;
+    const int left = n - i * R::kRows;
     if (idle) continue;
-    if (KW == 1) {
-      c.template fold<2>(k, k + Tl::kBytes, fa, hi, left, c2, nullptr);
+    if constexpr (KW == 1) {
+      c.template fold<R::kRows / 32>(k, k + R::kTile, fa, lane, left, c2);
     } else {
       const int half = wave >> 1;
-      if (left > half * 32) c.template fold<1>(k + half * 32 * RB, k + half * 32 * RB + Tl::kBytes, fa, hi, left - half * 32, c2, nullptr);
+      if (left > half * 32) c.template fold<1>(k + half * 32 * RB, k + half * 32 * RB + R::kTile, fa, lane, left - half * 32, c2);
     }
   }
+  wait_own_copies<0>();  // (the ring is about to be used for something else)
 }
 
 // ---------------------------------------------------------------- all slices
@@ -379,27 +429,34 @@ __device__ __forceinline__ void read_by_workgroup(Columns<D>& c, bool idle, cons
 // workgroup on the vector ALUs (1, 2, 4), or 0: by wave on the matrix pipe.
 template <int D, int PREFIX, int OWN>
 constexpr int slices_lds() {
-  return PREFIX > 0 || OWN == 0 ? 2 * 2 * 64 * D * 2 : kShWaves * OWN * (D + 2) * 4;
+  // the ring; or 32 rows of K and V of each wave, where their states go afterwards; or the waves' states of OWN heads
+  return PREFIX > 1 ? ring_bytes(D) : PREFIX == 1 || OWN == 0 ? kShWaves * 2 * 32 * D * 2 : kShWaves * OWN * (D + 2) * 4;
 }
+// (Three waves per SIMD at d = 64 with prefixes read by workgroups, of which two are resident first: own rows take the
+// third place at once.  512 queries behind 16384 rows 44.8 -> 42.5 us, own rows of 64 x 500, 64 heads on 8, 18.6 -> 16.8; without such
+// prefixes two are ahead, 33.5 / 36.0 us for 16 x 3100 rows.)
+constexpr int waves_per_simd(int d, int prefix) { return d == 64 && prefix > 1 ? 3 : 2; }
 template <int D, int PREFIX, int OWN>
-__global__ __launch_bounds__(kShWaves * 64, 2) void moda_shared_slices_kernel(SharedParams p) {
+__global__ __launch_bounds__(kShWaves * 64, waves_per_simd(D, PREFIX)) void moda_shared_slices_kernel(SharedParams p) {
   constexpr int RB = D * 2;
   constexpr bool kMatrix = PREFIX > 0 || OWN == 0;
+  constexpr int kAhead = D == 64 && waves_per_simd(D, PREFIX) == 2 ? 2 : 1;  // blocks in flight of a wave that reads by itself: registers
   __shared__ __attribute__((aligned(1024))) unsigned char smem[slices_lds<D, PREFIX, OWN>()];
   __shared__ float stat[kMatrix ? kShWaves : 1][32][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, hi = lane >> 5;
   const unsigned lds = (unsigned)(size_t)(lds_ptr)smem;
   const int G = p.Hq / p.Hk;
   const float c2 = p.scale_log2;
-  const size_t state = (size_t)p.n_slices * state_floats(D);  // of one head
   int id = blockIdx.x;
-  // a wave's part of the n rows of a slice: a quarter, in whole blocks of 32
-  auto part = [&](int n, int& first) {
-    const int q = ((n + kShWaves - 1) / kShWaves + 31) / 32 * 32;
-    first = min(wave * q, n);
-    return min(q, n - first);
+  // a wave's part of the rows of a run: a quarter, in whole blocks of 32
+  auto part = [&](int& n, const char*& K, const char*& V) {
+    const int q = ((n + kShWaves - 1) / kShWaves + 31) / 32 * 32, first = min(wave * q, n);
+    n = min(q, n - first);
+    K += (size_t)first * RB;
+    V += (size_t)first * RB;
+    return first;
   };
-  if (PREFIX > 0 && id < p.prefix_blocks) {
+  if (PREFIX > 0 && id < p.prefix_blocks) {  // (they last longest: they come first)
     const int per = p.B / p.Np, M = per * G;  // queries of a prefix and key/value head
     constexpr int CW = PREFIX > 0 ? PREFIX : 1, kCols = CW * 32;
     // column chunks of the same rows are neighbours on a die (ids equal mod 8), whose L2 then serves all but the first
@@ -416,60 +473,53 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_shared_slices_kernel(Sh
     c.init((const char*)p.Q + head_of(min(col0 + l32, M - 1)) * RB, hi);
     const int begin = slice * p.prefix_per, n = max(0, min(plen - begin, p.prefix_per));
     const size_t at = ((size_t)xg * p.P_alloc + begin) * RB;
-    const char *K = (const char*)p.Kp + at, *V = (const char*)p.Vp + at;
+    Rows x_rows = {(const char*)p.Kp + at, (const char*)p.Vp + at, n, nullptr, nullptr, 0};
     if constexpr (PREFIX == 1) {
-      int first;
-      const int mine = part(n, first);
-      read_by_wave<D>(c, K + (size_t)first * RB, V + (size_t)first * RB, mine, lds + wave * 2 * 32 * RB, c2, nullptr);
+      part(x_rows.n, x_rows.K, x_rows.V);
+      read_by_wave<D, kAhead>(c, x_rows, lds + wave * 2 * 32 * RB, c2);
     } else {
-      read_by_workgroup<D, kShWaves / CW>(c, col0 >= M, K, V, n, lds, c2);
+      read_by_workgroup<D, kShWaves / CW>(c, col0 >= M, x_rows.K, x_rows.V, n, lds, c2);
     }
-    fold_waves<D, CW>(c, smem, stat, c2, [&](int col) {
-      col += cc * kCols;
-      return col < M ? p.ws + head_of(col) * state + (size_t)slice * state_floats(D) : nullptr;
-    });
+    const size_t to = ((size_t)xg * p.n_prefix + slice) * M + cc * kCols;
+    fold_waves<D, CW>(c, smem, stat, c2, min(kCols, M - cc * kCols), p.ws_o + to * D, p.ws_ml + to * 2);
     return;
   }
   if (PREFIX > 0) id -= p.prefix_blocks;
-  // own rows: slices, then the depth slots
-  const int n_own = p.n_slices - p.n_prefix;
+  // own rows; the slots go with the last slice
   constexpr int kHeads = OWN > 0 ? OWN : 32;  // of a workgroup
-  const int slice = id % n_own, n_gc = (G + kHeads - 1) / kHeads;
-  id /= n_own;
+  const int slice = id % p.n_own, n_gc = (G + kHeads - 1) / kHeads;
+  id /= p.n_own;
   const int gc = id % n_gc, bg = id / n_gc, b = bg / p.Hk, g = bg - b * p.Hk;
   const int h0 = g * G + gc * kHeads, nh = min(kHeads, G - gc * kHeads);
-  const bool depth = slice == p.n_own;
-  const int begin = depth ? 0 : slice * p.own_per;
-  const int n = depth ? p.depth_count : max(0, min(filled(p.lengths, b, p.T) - begin, p.own_per));
-  const size_t at = ((size_t)bg * (depth ? p.depth_alloc : p.T_alloc) + begin) * RB;
-  const char *K = (const char*)(depth ? p.Kd : p.Ks) + at, *V = (const char*)(depth ? p.Vd : p.Vs) + at;
+  const int begin = slice * p.own_per;
+  const size_t at = ((size_t)bg * p.T_alloc + begin) * RB, slot_at = (size_t)bg * p.depth_alloc * RB;
+  Rows x = {(const char*)p.Ks + at, (const char*)p.Vs + at, max(0, min(filled(p.lengths, b, p.T) - begin, p.own_per)),
+            (const char*)p.Kd + slot_at, (const char*)p.Vd + slot_at, slice == p.n_own - 1 ? p.depth_count : 0};
   const size_t bh = (size_t)b * p.Hq + h0;
-  float* dst = p.ws + bh * state + (size_t)(p.n_prefix + slice) * state_floats(D);
-  const bool keep = p.w_out && !depth;
+  const size_t to = (size_t)p.B * p.Hq * p.n_prefix + ((size_t)bg * p.n_own + slice) * G + gc * kHeads;
   if constexpr (OWN > 0) {
-    read_rows<D, OWN>(K, V, n, (const char*)p.Q + bh * RB, nh, c2, dst, state, keep ? p.scores + bh * p.score_step + begin : nullptr,
-                      p.score_step, (float*)smem);
+    read_rows<D, OWN>(x, (const char*)p.Q + bh * RB, nh, c2, p.ws_o + to * D, p.ws_ml + to * 2,
+                      p.w_out ? p.scores + bh * p.score_step + begin : nullptr, p.score_step, (float*)smem);
   } else {
     Columns<D> c;
     const int j = min(l32, nh - 1);
     c.init((const char*)p.Q + (bh + j) * RB, hi);
-    int first;
-    const int mine = part(n, first);
-    read_by_wave<D>(c, K + (size_t)first * RB, V + (size_t)first * RB, mine, lds + wave * 2 * 32 * RB, c2,
-                    keep && l32 < nh ? p.scores + (bh + j) * p.score_step + begin + first : nullptr);
-    fold_waves<D, 1>(c, smem, stat, c2, [&](int col) { return col < nh ? dst + col * state : nullptr; });
+    const int first = part(x.n, x.K, x.V);
+    part(x.n2, x.K2, x.V2);
+    read_by_wave<D, kAhead>(c, x, lds + wave * 2 * 32 * RB, c2, p.w_out ? p.scores + bh * p.score_step + begin + first : nullptr, p.score_step, nh);
+    fold_waves<D, 1>(c, smem, stat, c2, nh, p.ws_o + to * D, p.ws_ml + to * 2);
   }
 }
 
 // ---------------------------------------------------------------- outputs
 // Workgroups [0, merge_blocks): O and LSE.  `by` slices of a head at a time, D / 4 threads each (four channels a thread), 1024 / D
 // such teams in a workgroup.  The others: weights_out of 1024 rows of one (batch, key/value head); each finds the LSE of
-// the group's heads from the slices' references and normalisers (8 bytes of a state).
-constexpr int kFinishRows = 1024, kFinishHeads = 64;
+// the group's heads from the slices' references and normalisers (8 bytes a state).
+constexpr int kFinishRows = 1024;
 template <int D>
 __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p, int by, int merge_blocks, int n_chunks) {
   constexpr int kTeam = D / 4, kTeams = 256 / kTeam;
-  __shared__ __attribute__((aligned(16))) float red[kTeams][state_floats(D)];
+  __shared__ __attribute__((aligned(16))) float red[kTeams][D + 4];
   const float c2 = p.scale_log2;
   const int tid = threadIdx.x;
   // (a state whose scores are all -inf is empty: reference -inf, weight zero)
@@ -479,16 +529,17 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
     const long long bh = (long long)blockIdx.x * (kTeams / by) + team / by, heads = (long long)p.B * p.Hq;
     float mm = -INFINITY, ll = 0.f;
     f32x4 oo = {0.f, 0.f, 0.f, 0.f};
-    const float* ws = p.ws + (size_t)min(bh, heads - 1) * p.n_slices * state_floats(D);
+    const int row = (int)min(bh, heads - 1), b = row / p.Hq, h = row % p.Hq, G = p.Hq / p.Hk;
+    const HeadStates at(p, b, h / G, h % G);
     constexpr int kU = 4;
     for (int s0 = part; s0 < p.n_slices; s0 += kU * by) {
       f32x2 st[kU];
       f32x4 o[kU];
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
-        const float* x = ws + (size_t)min(s0 + u * by, p.n_slices - 1) * state_floats(D);
-        st[u] = *(const f32x2*)(x + D);
-        o[u] = *(const f32x4*)(x + ch);
+        const size_t i = at(p, min(s0 + u * by, p.n_slices - 1));
+        st[u] = *(const f32x2*)(p.ws_ml + i * 2);
+        o[u] = *(const f32x4*)(p.ws_o + i * D + ch);
       }
       float mn = mm;
 #pragma unroll
@@ -535,95 +586,96 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
     return;
   }
   const int id = blockIdx.x - merge_blocks, bg = id / n_chunks, j0 = id % n_chunks * kFinishRows;
-  const int b = bg / p.Hk, g = bg - b * p.Hk, G = p.Hq / p.Hk, lane = tid & 63;
+  const int b = bg / p.Hk, g = bg - b * p.Hk, G = p.Hq / p.Hk;
   const int len = filled(p.lengths, b, p.T);
   if (j0 >= len) return;
-  constexpr int kRows = kFinishRows / 256;
-  const size_t row = (size_t)bg * p.T_alloc;
-  float w[kRows];
+  // four rows a thread, eight heads at a time: their logits are asked for before the LSE is known
+  const int j = j0 + tid * 4;
+  const size_t row = (size_t)bg * p.T_alloc + j;
+  float w[4];
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int j = min(j0 + i * 256 + tid, len - 1);
-    w[i] = p.w_in ? p.w_in[row + j] : 0.f;
-  }
-  float* lse2 = &red[0][0];  // LSE * log2(e) of kFinishHeads heads; +inf where nothing has weight
-  static_assert(kFinishHeads <= kTeams * state_floats(D), "");
-  for (int h0 = 0; h0 < G; h0 += kFinishHeads) {
-    const int nh = min(kFinishHeads, G - h0);
+  for (int i = 0; i < 4; ++i) w[i] = p.w_in && j + i < len ? p.w_in[row + i] : 0.f;
+  float* lse2 = &red[0][0];  // LSE * log2(e) of eight heads; +inf where nothing has weight
+  const int at_row = min(j, (int)p.score_step - 4);  // (what lies behind the sequence is not stored)
+  const float* sc = p.scores + ((size_t)b * p.Hq + g * G) * p.score_step + at_row;
+  for (int h0 = 0; h0 < G; h0 += 8) {
+    f32x4 s[8];
+#pragma unroll
+    for (int h = 0; h < 8; ++h) s[h] = *(const f32x4*)(sc + (size_t)min(h0 + h, G - 1) * p.score_step);
     __syncthreads();
-    for (int h = tid >> 6; h < nh; h += 4) {  // a wave per head
-      const float* ws = p.ws + ((size_t)b * p.Hq + g * G + h0 + h) * p.n_slices * state_floats(D) + D;
+    {  // 32 lanes per head
+      const int h = tid >> 5;
+      const HeadStates at(p, b, g, min(h0 + h, G - 1));
       float m = -INFINITY, l = 0.f;
-      for (int s = lane; s < p.n_slices; s += 64) {
-        const f32x2 x = *(const f32x2*)(ws + (size_t)s * state_floats(D));
+      for (int i = tid & 31; i < p.n_slices; i += 32) {
+        const f32x2 x = *(const f32x2*)(p.ws_ml + at(p, i) * 2);
         const float mn = fmaxf(m, x[0]);
         l = l * factor(m, mn) + factor(x[0], mn) * x[1];
         m = mn;
       }
 #pragma unroll
-      for (int x = 1; x < 64; x *= 2) {
+      for (int x = 1; x < 32; x *= 2) {
         const float m2 = __shfl_xor(m, x), l2 = __shfl_xor(l, x), mn = fmaxf(m, m2);
         l = l * factor(m, mn) + l2 * factor(m2, mn);
         m = mn;
       }
-      if (lane == 0) lse2[h] = l == 0.f ? INFINITY : m * c2 + __log2f(l);
+      if ((tid & 31) == 0) lse2[h] = h0 + h >= G || l == 0.f ? INFINITY : m * c2 + __log2f(l);
     }
     __syncthreads();
-    const float* sc = p.scores + ((size_t)b * p.Hq + g * G + h0) * p.score_step;
-    for (int h = 0; h < nh; ++h) {
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+      if (h0 + h >= G) break;  // (uniform)
       const float z = lse2[h];
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const int j = min(j0 + i * 256 + tid, len - 1);
-        w[i] += fast_exp2(__builtin_fmaf(sc[h * p.score_step + j], c2, -z));
-      }
+      for (int i = 0; i < 4; ++i) w[i] += fast_exp2(__builtin_fmaf(s[h][i], c2, -z));
     }
   }
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int j = j0 + i * 256 + tid;
-    if (j < len) p.w_out[row + j] = w[i];
-  }
+  for (int i = 0; i < 4; ++i)
+    if (j + i < len) p.w_out[row + i] = w[i];
 }
 
 // ---------------------------------------------------------------- the cut into slices
 static int own_kind(int G) { return G > 4 ? 0 : G >= 3 ? 4 : G; }
 
-static void plan(SharedParams& p) {
+// Slices of a run of `rows` rows that `units` workgroups read each.  Long runs: `many` workgroups in all, which the chip holds at
+// once, as long as a slice has `good` rows; a second round of workgroups costs a workgroup's chain of latencies again, about
+// 5 us.  Runs that leave units without work: one workgroup per unit down to `least` rows, what the waves take at a time.
+static void cut(int rows, long long units, int many, int good, int least, int& n, int& per) {
+  auto most = [&](int size) { return ((long long)rows + size - 1) / size; };
+  long long want = std::max(std::min(256 / units, most(least)), std::min(many / units, most(good)));
+  want = std::max(std::max(want, 1ll), ((long long)rows >> 22) + 1);  // (a slice is addressed with 32-bit byte offsets)
+  per = (int)((rows + want - 1) / want + least - 1) / least * least;
+  n = per > 0 ? (rows + per - 1) / per : 0;
+}
+
+static void plan(SharedParams& p, int d) {
   const int G = p.Hq / p.Hk;
-  const long long M = (long long)p.B / p.Np * G;
-  auto cut = [](int rows, long long want, int least, int step, int& n, int& per) {
-    want = std::max(want, ((long long)rows >> 22) + 1);  // (a slice is addressed with 32-bit byte offsets)
-    n = (int)std::min(want, ((long long)rows + least - 1) / least);
-    per = n > 0 ? (int)((((long long)rows + n - 1) / n + step - 1) / step * step) : 0;
-    n = n > 0 ? (rows + per - 1) / per : 0;
-  };
-  // prefixes: two workgroups of four waves per compute unit
+  const long long M = (long long)p.B / p.Np * G, xg = (long long)p.Np * p.Hk, groups = (long long)p.B * p.Hk;
   p.prefix_kind = p.P == 0 ? 0 : M <= 32 ? 1 : M <= 64 ? 2 : 4;
-  p.n_prefix = p.prefix_per = 0;
-  long long blocks = 0;
+  p.n_prefix = p.prefix_per = p.prefix_blocks = 0;
   if (p.P > 0) {
-    const long long xg = (long long)p.Np * p.Hk, cc = (M + p.prefix_kind * 32 - 1) / (p.prefix_kind * 32);
-    if (p.prefix_kind == 1) cut(p.P, std::max(1ll, 768 / xg), 128, 128, p.n_prefix, p.prefix_per);
-    else cut(p.P, std::max(1ll, 512 / (xg * cc)), 256, 64, p.n_prefix, p.prefix_per);
-    blocks = (xg * p.n_prefix + 7) / 8 * 8 * cc;
+    // (by wave: as many again come with the own rows.  32 columns behind 32768 rows, 16 heads: 256 workgroups 84.8 us, 768 93.8;
+    // 64 heads of 2000 rows 19.5 / 25.8)
+    const long long cc = (M + p.prefix_kind * 32 - 1) / (p.prefix_kind * 32);
+    if (p.prefix_kind == 1) cut(p.P, xg, 256, 512, 128, p.n_prefix, p.prefix_per);
+    else cut(p.P, xg * cc, 512, 256, 64, p.n_prefix, p.prefix_per);
+    const long long blocks = (xg * p.n_prefix + 7) / 8 * 8 * cc;
+    p.prefix_blocks = blocks > 0x7fffffff ? 0x7fffffff : (int)blocks;  // (too many: the launch is refused)
   }
-  p.prefix_blocks = blocks > 0x7fffffff ? 0x7fffffff : (int)blocks;  // (too many: the launch is refused)
-  const long long groups = (long long)p.B * p.Hk;
-  if (own_kind(G) > 0) cut(p.T, std::max(1ll, 2048 / groups), 256, 64, p.n_own, p.own_per);
-  else cut(p.T, std::max(1ll, 768 / (groups * ((G + 31) / 32))), 128, 128, p.n_own, p.own_per);
-  p.n_slices = p.n_prefix + p.n_own + (p.depth_count > 0 ? 1 : 0);
+  if (own_kind(G) > 0) cut(p.T, groups, 512, 256, kShWaves * 4 * 512 / d, p.n_own, p.own_per);
+  else cut(p.T, groups * ((G + 31) / 32), 512, 512, 128, p.n_own, p.own_per);
+  if (p.depth_count > 0) p.n_own = std::max(p.n_own, 1);
+  p.n_slices = p.n_prefix + p.n_own;
   p.score_step = ((size_t)p.T + 31) / 32 * 32;
 }
 
-static size_t state_bytes(const SharedParams& p, int d) {
-  return ((size_t)p.B * p.Hq * p.n_slices * state_floats(d) * sizeof(float) + 15) / 16 * 16;
-}
+static size_t states(const SharedParams& p) { return ((size_t)p.B * p.Hq * p.n_slices + 1) / 2 * 2; }  // (even: 16-byte pieces)
 
 size_t decode_shared_workspace_bytes(const SharedParams& dims, int d, bool with_weights) {
   SharedParams p = dims;
-  plan(p);
-  const size_t bytes = state_bytes(p, d) + (with_weights ? (size_t)p.B * p.Hq * p.score_step * sizeof(float) : 0);
+  plan(p, d);
+  const size_t bytes = (states(p) * (d + 2) + (with_weights ? (size_t)p.B * p.Hq * p.score_step : 0)) * sizeof(float);
   return std::max<size_t>(bytes, 16);
 }
 
@@ -635,9 +687,9 @@ static void (*slices_kernel(int own))(SharedParams) {
 
 template <int D>
 static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
-  const int G = p.Hq / p.Hk, own = own_kind(G), n_own = p.n_slices - p.n_prefix;
+  const int G = p.Hq / p.Hk, own = own_kind(G);
   const int heads_per = own > 0 ? own : 32;
-  const long long blocks = p.prefix_blocks + (long long)p.B * p.Hk * ((G + heads_per - 1) / heads_per) * n_own;
+  const long long blocks = p.prefix_blocks + (long long)p.B * p.Hk * ((G + heads_per - 1) / heads_per) * p.n_own;
   // teams of a workgroup that share a head's slices, so that each folds four or fewer of them at a time
   const int teams = 1024 / D;
   int by = 1;
@@ -656,9 +708,10 @@ static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_decode_shared(SharedParams p, int d, void* workspace, hipStream_t stream) {
-  plan(p);
-  p.ws = (float*)workspace;
-  p.scores = (float*)((char*)workspace + state_bytes(p, d));
+  plan(p, d);
+  p.ws_o = (float*)workspace;
+  p.ws_ml = p.ws_o + states(p) * d;
+  p.scores = p.ws_ml + states(p) * 2;
   return d == 128 ? launch_d<128>(p, stream) : launch_d<64>(p, stream);
 }
 

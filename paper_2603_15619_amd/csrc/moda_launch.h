@@ -81,7 +81,8 @@ struct SharedParams {
   float* w_out;               // the same, or null
   void* O;
   float* LSE;
-  float* ws;      // [B, Hq, n_slices, d + 2]
+  float* ws_o;    // [states, d], states = B * Hq * n_slices: unnormalised outputs
+  float* ws_ml;   // [states, 2]: references (logits before the scale) and normalisers
   float* scores;  // [B, Hq, score_step] (with w_out): logits of the own rows, before the scale
   size_t score_step;
   int B, Hq, Hk, T, T_alloc;
@@ -89,8 +90,8 @@ struct SharedParams {
   int depth_alloc, depth_count;
   int prefix_kind, prefix_blocks;  // how prefixes are read, by how many workgroups
   int n_prefix, prefix_per;  // slices of a prefix, rows of one
-  int n_own, own_per;        // slices of an own cache, rows of one
-  int n_slices;              // both, and one for the depth slots where there are any
+  int n_own, own_per;        // slices of an own cache, rows of one; the slots go with the last (at least one, with slots)
+  int n_slices;              // both
   float scale, scale_log2;
 };
 size_t decode_shared_workspace_bytes(const SharedParams& p, int d, bool with_weights);
