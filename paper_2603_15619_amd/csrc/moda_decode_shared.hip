@@ -10,7 +10,7 @@
 //
 // One launch takes all slices:
 //   prefixes   all queries that share a prefix (sequences x heads of a group) are the columns of matrix products
-//              S^T = K Q^T, O^T += V^T P^T.  Up to 32 columns (read_by_wave): every wave reads its own part of the slice.
+//              S^T = K Q^T, O^T += V^T P^T; up to 4 take the vector ALUs (read_rows).  Up to 32 (read_by_wave): every wave reads its own part of the slice.
 //              More (read_by_workgroup): 2 or 4 waves of 32 columns share the K and V tiles of a slice in LDS.
 //   own rows   up to 4 heads per group on the vector ALUs (read_rows), more as the columns of read_by_wave.
 #include <algorithm>
@@ -55,10 +55,10 @@ __device__ __forceinline__ int filled(const int* lengths, int i, int most) {
 
 // ---------------------------------------------------------------- rows on the vector ALUs
 // A lane owns 8 channels, d/8 lanes a row; a wave takes kU batches of 64 / (d/8) rows at a time, the next ones in
-// flight, and raises its reference once for them.  `q` = GT query rows (heads from nh on repeat the last one and are not
-// stored), `o_out`, `ml_out` = the first head's state, `scores` = the first head's logits of the first run, or null.
-template <int D, int GT>
-__device__ __forceinline__ void read_rows(const Rows& x, const char* q_rows, int nh, float c2, float* o_out,
+// flight, and raises its reference once for them.  query(j) = the address of query j of GT (from nh on the last one repeats and is
+// not stored), `o_out`, `ml_out` = the first query's state, `scores` = the first one's logits of the first run, or null.
+template <int D, int GT, class Query>
+__device__ __forceinline__ void read_rows(const Rows& x, Query&& query, int nh, float c2, float* o_out,
                                           float* ml_out, float* scores, size_t score_step, float* red) {
   constexpr int LPR = D / 8, RPS = 64 / LPR, RB = D * 2, kU = 4, STEP = kShWaves * kU * RPS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = lane / LPR, l16 = lane % LPR;
@@ -66,7 +66,7 @@ __device__ __forceinline__ void read_rows(const Rows& x, const char* q_rows, int
   float m[GT], l[GT], o[GT][8];
 #pragma unroll
   for (int j = 0; j < GT; ++j) {
-    q[j] = *(const u32x4*)(q_rows + (size_t)min(j, nh - 1) * RB + l16 * 16);
+    q[j] = *(const u32x4*)(query(min(j, nh - 1)) + l16 * 16);
     m[j] = -INFINITY;
     l[j] = 0.f;
 #pragma unroll
@@ -425,21 +425,22 @@ __device__ __forceinline__ void read_by_workgroup(Columns<D>& c, bool idle, cons
 }
 
 // ---------------------------------------------------------------- all slices
-// PREFIX: how prefixes are read (0: none, 1: by wave, 2 / 4: by workgroup, so many waves of columns).  OWN: heads per
+// PREFIX: how prefixes are read (0: none, 1: by wave, 2 / 4: by workgroup, so many waves of columns, 3: vector ALUs).  OWN: heads per
 // workgroup on the vector ALUs (1, 2, 4), or 0: by wave on the matrix pipe.
 template <int D, int PREFIX, int OWN>
 constexpr int slices_lds() {
   // the ring; or 32 rows of K and V of each wave, where their states go afterwards; or the waves' states of OWN heads
-  return PREFIX > 1 ? ring_bytes(D) : PREFIX == 1 || OWN == 0 ? kShWaves * 2 * 32 * D * 2 : kShWaves * OWN * (D + 2) * 4;
+  return PREFIX == 2 || PREFIX == 4 ? ring_bytes(D) : PREFIX == 1 || OWN == 0 ? kShWaves * 2 * 32 * D * 2
+         : kShWaves * (PREFIX == 3 ? 4 : OWN) * (D + 2) * 4;
 }
 // (Three waves per SIMD at d = 64 with prefixes read by workgroups, of which two are resident first: own rows take the
 // third place at once.  512 queries behind 16384 rows 44.8 -> 42.5 us, own rows of 64 x 500, 64 heads on 8, 18.6 -> 16.8; without such
 // prefixes two are ahead, 33.5 / 36.0 us for 16 x 3100 rows.)
-constexpr int waves_per_simd(int d, int prefix) { return d == 64 && prefix > 1 ? 3 : 2; }
+constexpr int waves_per_simd(int d, int prefix) { return d == 64 && (prefix == 2 || prefix == 4) ? 3 : 2; }
 template <int D, int PREFIX, int OWN>
 __global__ __launch_bounds__(kShWaves * 64, waves_per_simd(D, PREFIX)) void moda_shared_slices_kernel(SharedParams p) {
   constexpr int RB = D * 2;
-  constexpr bool kMatrix = PREFIX > 0 || OWN == 0;
+  constexpr bool kMatrix = (PREFIX > 0 && PREFIX != 3) || OWN == 0;
   constexpr int kAhead = D == 64 && waves_per_simd(D, PREFIX) == 2 ? 2 : 1;  // blocks in flight of a wave that reads by itself: registers
   __shared__ __attribute__((aligned(1024))) unsigned char smem[slices_lds<D, PREFIX, OWN>()];
   __shared__ float stat[kMatrix ? kShWaves : 1][32][2];
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(kShWaves * 64, waves_per_simd(D, PREFIX)) void moda
   };
   if (PREFIX > 0 && id < p.prefix_blocks) {  // (they last longest: they come first)
     const int per = p.B / p.Np, M = per * G;  // queries of a prefix and key/value head
-    constexpr int CW = PREFIX > 0 ? PREFIX : 1, kCols = CW * 32;
+    constexpr int CW = PREFIX > 0 && PREFIX != 3 ? PREFIX : 1, kCols = CW * 32;
     // column chunks of the same rows are neighbours on a die (ids equal mod 8), whose L2 then serves all but the first
     const int n_cc = (M + kCols - 1) / kCols;
     const int u = id / (8 * n_cc) * 8 + id % 8, cc = id / 8 % n_cc;
@@ -468,19 +469,24 @@ __global__ __launch_bounds__(kShWaves * 64, waves_per_simd(D, PREFIX)) void moda
     const int plen = filled(p.prefix_lengths, x, p.P);
     // column -> (sequence of the prefix, head of the group); a column past the last repeats it and is not stored
     auto head_of = [&](int col) { return (size_t)(x * per + col / G) * p.Hq + g * G + col % G; };
-    const int col0 = cc * kCols + (wave % CW) * 32;
-    Columns<D> c;
-    c.init((const char*)p.Q + head_of(min(col0 + l32, M - 1)) * RB, hi);
     const int begin = slice * p.prefix_per, n = max(0, min(plen - begin, p.prefix_per));
     const size_t at = ((size_t)xg * p.P_alloc + begin) * RB;
     Rows x_rows = {(const char*)p.Kp + at, (const char*)p.Vp + at, n, nullptr, nullptr, 0};
+    const size_t to = ((size_t)xg * p.n_prefix + slice) * M + cc * kCols;
+    if constexpr (PREFIX == 3) {
+      read_rows<D, 4>(x_rows, [&](int j) { return (const char*)p.Q + head_of(j) * RB; }, M, c2, p.ws_o + to * D, p.ws_ml + to * 2,
+                      nullptr, 0, (float*)smem);
+      return;
+    }
+    const int col0 = cc * kCols + (wave % CW) * 32;
+    Columns<D> c;
+    c.init((const char*)p.Q + head_of(min(col0 + l32, M - 1)) * RB, hi);
     if constexpr (PREFIX == 1) {
       part(x_rows.n, x_rows.K, x_rows.V);
       read_by_wave<D, kAhead>(c, x_rows, lds + wave * 2 * 32 * RB, c2);
     } else {
       read_by_workgroup<D, kShWaves / CW>(c, col0 >= M, x_rows.K, x_rows.V, n, lds, c2);
     }
-    const size_t to = ((size_t)xg * p.n_prefix + slice) * M + cc * kCols;
     fold_waves<D, CW>(c, smem, stat, c2, min(kCols, M - cc * kCols), p.ws_o + to * D, p.ws_ml + to * 2);
     return;
   }
@@ -498,7 +504,7 @@ __global__ __launch_bounds__(kShWaves * 64, waves_per_simd(D, PREFIX)) void moda
   const size_t bh = (size_t)b * p.Hq + h0;
   const size_t to = (size_t)p.B * p.Hq * p.n_prefix + ((size_t)bg * p.n_own + slice) * G + gc * kHeads;
   if constexpr (OWN > 0) {
-    read_rows<D, OWN>(x, (const char*)p.Q + bh * RB, nh, c2, p.ws_o + to * D, p.ws_ml + to * 2,
+    read_rows<D, OWN>(x, [&](int j) { return (const char*)p.Q + (bh + j) * RB; }, nh, c2, p.ws_o + to * D, p.ws_ml + to * 2,
                       p.w_out ? p.scores + bh * p.score_step + begin : nullptr, p.score_step, (float*)smem);
   } else {
     Columns<D> c;
@@ -592,9 +598,17 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
   // four rows a thread, eight heads at a time: their logits are asked for before the LSE is known
   const int j = j0 + tid * 4;
   const size_t row = (size_t)bg * p.T_alloc + j;
-  float w[4];
+  const bool whole = p.T_alloc % 4 == 0 && j + 4 <= len;  // (16-byte aligned then)
+  f32x4 w = {0.f, 0.f, 0.f, 0.f};
+  if (p.w_in) {
+    if (whole) {
+      w = *(const f32x4*)(p.w_in + row);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = p.w_in && j + i < len ? p.w_in[row + i] : 0.f;
+      for (int i = 0; i < 4; ++i)
+        if (j + i < len) w[i] = p.w_in[row + i];
+    }
+  }
   float* lse2 = &red[0][0];  // LSE * log2(e) of eight heads; +inf where nothing has weight
   const int at_row = min(j, (int)p.score_step - 4);  // (what lies behind the sequence is not stored)
   const float* sc = p.scores + ((size_t)b * p.Hq + g * G) * p.score_step + at_row;
@@ -630,9 +644,13 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
       for (int i = 0; i < 4; ++i) w[i] += fast_exp2(__builtin_fmaf(s[h][i], c2, -z));
     }
   }
+  if (whole) {
+    *(f32x4*)(p.w_out + row) = w;
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (j + i < len) p.w_out[row + i] = w[i];
+    for (int i = 0; i < 4; ++i)
+      if (j + i < len) p.w_out[row + i] = w[i];
+  }
 }
 
 // ---------------------------------------------------------------- the cut into slices
@@ -652,13 +670,14 @@ static void cut(int rows, long long units, int many, int good, int least, int& n
 static void plan(SharedParams& p, int d) {
   const int G = p.Hq / p.Hk;
   const long long M = (long long)p.B / p.Np * G, xg = (long long)p.Np * p.Hk, groups = (long long)p.B * p.Hk;
-  p.prefix_kind = p.P == 0 ? 0 : M <= 32 ? 1 : M <= 64 ? 2 : 4;
+  p.prefix_kind = p.P == 0 ? 0 : M <= 4 ? 3 : M <= 32 ? 1 : M <= 64 ? 2 : 4;
   p.n_prefix = p.prefix_per = p.prefix_blocks = 0;
   if (p.P > 0) {
     // (by wave: as many again come with the own rows.  32 columns behind 32768 rows, 16 heads: 256 workgroups 84.8 us, 768 93.8;
     // 64 heads of 2000 rows 19.5 / 25.8)
     const long long cc = (M + p.prefix_kind * 32 - 1) / (p.prefix_kind * 32);
-    if (p.prefix_kind == 1) cut(p.P, xg, 256, 512, 128, p.n_prefix, p.prefix_per);
+    if (p.prefix_kind == 3) cut(p.P, xg, 512, 256, kShWaves * 4 * 512 / d, p.n_prefix, p.prefix_per);
+    else if (p.prefix_kind == 1) cut(p.P, xg, 256, 512, 128, p.n_prefix, p.prefix_per);
     else cut(p.P, xg * cc, 512, 256, 64, p.n_prefix, p.prefix_per);
     const long long blocks = (xg * p.n_prefix + 7) / 8 * 8 * cc;
     p.prefix_blocks = blocks > 0x7fffffff ? 0x7fffffff : (int)blocks;  // (too many: the launch is refused)
@@ -681,7 +700,9 @@ size_t decode_shared_workspace_bytes(const SharedParams& dims, int d, bool with_
 
 template <int D, int PREFIX>
 static void (*slices_kernel(int own))(SharedParams) {
-  return own == 4 ? moda_shared_slices_kernel<D, PREFIX, 4> : own == 2 ? moda_shared_slices_kernel<D, PREFIX, 2>
+  if constexpr (PREFIX == 3)  // (4 queries at most: so are the heads of a group)
+    return own == 4 ? moda_shared_slices_kernel<D, 3, 4> : own == 2 ? moda_shared_slices_kernel<D, 3, 2> : moda_shared_slices_kernel<D, 3, 1>;
+  else return own == 4 ? moda_shared_slices_kernel<D, PREFIX, 4> : own == 2 ? moda_shared_slices_kernel<D, PREFIX, 2>
          : own == 1 ? moda_shared_slices_kernel<D, PREFIX, 1> : moda_shared_slices_kernel<D, PREFIX, 0>;
 }
 
@@ -700,7 +721,7 @@ static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
   if ((blocks > 0 && !grid_ok(blocks, kShWaves * 64)) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
   if (blocks > 0) {
     auto* kernel = p.prefix_kind == 0 ? slices_kernel<D, 0>(own) : p.prefix_kind == 1 ? slices_kernel<D, 1>(own)
-                   : p.prefix_kind == 2 ? slices_kernel<D, 2>(own) : slices_kernel<D, 4>(own);
+                   : p.prefix_kind == 2 ? slices_kernel<D, 2>(own) : p.prefix_kind == 3 ? slices_kernel<D, 3>(own) : slices_kernel<D, 4>(own);
     const hipError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kShWaves * 64), stream, p);
     if (e != hipSuccess) return e;
   }
