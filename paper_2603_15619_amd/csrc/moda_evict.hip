@@ -8,37 +8,25 @@
 //          and a hole below it, so no row is both read and written, in whatever order the workgroups run.
 #include <algorithm>
 
+#include "moda_evict.h"
 #include "moda_launch.h"
 
 namespace moda {
 
 constexpr int kEvThreads = 1024, kEvWaves = kEvThreads / 64;
 
-// Orders as the float does; -0 as 0, a NaN below everything.
-__device__ __forceinline__ unsigned weight_key(float w) {
-  const unsigned u = __builtin_bit_cast(unsigned, w + 0.f);
-  return w != w ? 0u : u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
-}
-
-// Workspace of the long caches: bits and list of every (sequence, head).
-struct EvictScratch {
-  unsigned long long* bits;
-  size_t words;  // of one
-  int* list;
-};
-
-// Rows of a (sequence, head): wave w takes `steps` times 64 of them, from w * steps * 64 on.  N > 0: steps = N, and a row's key stays in
-// a register from its one read on; 0: as many steps as it takes, and every pass reads weights and positions again.
+// Rows of a (sequence, head): wave w takes N times 64 of them, from w * N * 64 on; a row's key stays in a register from its one
+// read on.
 template <int N>
-__global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictParams p, EvictScratch ws) {
+__global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictParams p) {
   constexpr int kBins = 2048;
   __shared__ unsigned hist[kBins];
   __shared__ int part[kEvWaves], part2[kEvWaves];
   __shared__ unsigned s_digit;
   __shared__ int s_need;
   // rows that stay, a bit each; rows that move, in ascending order (half of all at most: as many as there are holes)
-  __shared__ unsigned long long lds_bits[N > 0 ? kEvWaves * N : 1];
-  __shared__ unsigned short lds_list[N > 0 ? kEvThreads * N / 2 : 1];
+  __shared__ unsigned long long bits[kEvWaves * N];
+  __shared__ unsigned short list[kEvThreads * N / 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bg = blockIdx.x, b = bg / p.Hk;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
@@ -51,21 +39,14 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   }
   const float* w = p.w + (size_t)bg * p.T_alloc;
   const int* pos = p.positions ? p.positions + (size_t)bg * p.T_alloc : nullptr;
-  const int steps = N > 0 ? N : (len + kEvThreads - 1) / kEvThreads;
-  const int r0 = wave * steps * 64 + lane;  // the lane's rows: r0 + 64 i
-  auto* bits = [&] { if constexpr (N > 0) return lds_bits; else return ws.bits + (size_t)bg * ws.words; }();
-  auto* list = [&] { if constexpr (N > 0) return lds_list; else return ws.list + (size_t)bg * p.n; }();
-  unsigned keys[N > 0 ? N : 1];
-  // N > 0: bounds-checked loads from one address register; rows past the end read as 0
-  const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc((void*)w, 0, N > 0 ? len * 4 : 0, 0x00020000);
-  const __amdgpu_buffer_rsrc_t pos_buf = __builtin_amdgcn_make_buffer_rsrc((void*)pos, 0, N > 0 && pos ? len * 4 : 0, 0x00020000);
+  const int r0 = wave * N * 64 + lane;  // the lane's rows: r0 + 64 i
+  unsigned keys[N];
+  // bounds-checked loads from one address register; rows past the end read as 0
+  const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc((void*)w, 0, len * 4, 0x00020000);
+  const __amdgpu_buffer_rsrc_t pos_buf = __builtin_amdgcn_make_buffer_rsrc((void*)pos, 0, pos ? len * 4 : 0, 0x00020000);
   auto each = [&](auto&& f) {  // f(i) for every step
-    if constexpr (N > 0) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) f(i);
-    } else {
-      for (int i = 0; i < steps; ++i) f(i);
-    }
+    for (int i = 0; i < N; ++i) f(i);
   };
 
   long long above = 0x7fffffffLL;  // rows whose position is above this are recent
@@ -75,9 +56,8 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
     if (pos) {
       newest = (int)0x80000000;
       each([&](int i) {
-        int x;
-        if constexpr (N > 0) keys[i] = (unsigned)(x = __builtin_amdgcn_raw_buffer_load_b32(pos_buf, r0 * 4, i * 256, 0));
-        else x = pos[min(r0 + i * 64, len - 1)];
+        const int x = __builtin_amdgcn_raw_buffer_load_b32(pos_buf, r0 * 4, i * 256, 0);
+        keys[i] = (unsigned)x;
         if (r0 + i * 64 < len) newest = max(newest, x);
       });
 #pragma unroll
@@ -90,19 +70,11 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
     }
     above = (long long)newest - p.recent;
   }
-  auto make_key = [&](int i) {
-    if constexpr (N > 0) {
-      const int at = by_position ? (int)keys[i] : r0 + i * 64;
-      const unsigned k = weight_key(__builtin_bit_cast(float, (unsigned)__builtin_amdgcn_raw_buffer_load_b32(w_buf, r0 * 4, i * 256, 0)));
-      return at > above ? 0xffffffffu : k;
-    } else {
-      const int r = min(r0 + i * 64, len - 1);
-      const unsigned k = weight_key(w[r]);
-      return (by_position ? pos[r] : r) > above ? 0xffffffffu : k;
-    }
-  };
-  if constexpr (N > 0) each([&](int i) { keys[i] = make_key(i); });
-  auto key_of = [&](int i) { return N > 0 ? keys[N > 0 ? i : 0] : make_key(i); };
+  each([&](int i) {
+    const int at = by_position ? (int)keys[i] : r0 + i * 64;
+    const unsigned k = weight_key(__builtin_bit_cast(float, (unsigned)__builtin_amdgcn_raw_buffer_load_b32(w_buf, r0 * 4, i * 256, 0)));
+    keys[i] = at > above ? 0xffffffffu : k;
+  });
 
   // the key of the fit-th row from the top, and how many of the rows with just that key stay: 11, 11 and 10 bits
   unsigned threshold = 0;
@@ -112,7 +84,7 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
     for (int i = tid; i < kBins; i += kEvThreads) hist[i] = 0;
     __syncthreads();
     each([&](int i) {
-      const unsigned k = key_of(i);
+      const unsigned k = keys[i];
       const bool in = r0 + i * 64 < len && (k & mask) == threshold;
       const unsigned bin = (k >> shift) & (kBins - 1);
       // many rows share a digit (equal weights, recent rows): those that share the first lane's are counted at once
@@ -157,7 +129,7 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
     return n;
   };
   int ties = 0;
-  each([&](int i) { ties += __popcll(__ballot(r0 + i * 64 < len && key_of(i) == threshold)); });
+  each([&](int i) { ties += __popcll(__ballot(r0 + i * 64 < len && keys[i] == threshold)); });
   if (lane == 0) part[wave] = ties;
   __syncthreads();
   const int ties_before = before(part);
@@ -166,13 +138,13 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   int seen = ties_before, holes = 0, movers = 0;
   each([&](int i) {
     const int r = r0 + i * 64, base = r - lane;
-    const unsigned k = key_of(i);
+    const unsigned k = keys[i];
     const unsigned long long tie = __ballot(r < len && k == threshold);
     unsigned long long stay = __ballot(r < len && k > threshold);
     if (seen + __popcll(tie) <= need) stay |= tie;
     else stay |= __ballot(((tie >> lane) & 1) && seen + __popcll(tie & below) < need);
     seen += __popcll(tie);
-    if (lane == 0) bits[wave * steps + i] = stay;
+    if (lane == 0) bits[wave * N + i] = stay;
     const unsigned long long low = fit - base >= 64 ? ~0ull : fit <= base ? 0ull : (1ull << (fit - base)) - 1;
     holes += __popcll(low & ~stay);
     movers += __popcll(stay & ~low);
@@ -184,10 +156,10 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   __syncthreads();
   int nth = before(part2);
 #pragma unroll 4
-  for (int i = 0; i < steps; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int r = r0 + i * 64, base = r - lane;
     if (base + 64 <= fit) continue;  // (uniform)
-    const unsigned long long stay = bits[wave * steps + i];
+    const unsigned long long stay = bits[wave * N + i];
     const unsigned long long mv = fit <= base ? stay : stay & ~((1ull << (fit - base)) - 1);
     if ((mv >> lane) & 1) list[nth + __popcll(mv & below)] = r;
     nth += __popcll(mv);
@@ -195,10 +167,10 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   __syncthreads();
   nth = before(part);
 #pragma unroll 4
-  for (int i = 0; i < steps; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int r = r0 + i * 64, base = r - lane;
     if (base >= fit) continue;  // (uniform)
-    const unsigned long long stay = bits[wave * steps + i], low = fit - base >= 64 ? ~0ull : (1ull << (fit - base)) - 1;
+    const unsigned long long stay = bits[wave * N + i], low = fit - base >= 64 ? ~0ull : (1ull << (fit - base)) - 1;
     const unsigned long long hole = low & ~stay;
     if (r < fit) index[r] = ((hole >> lane) & 1) ? list[nth + __popcll(hole & below)] : r;
     nth += __popcll(hole);
@@ -243,13 +215,11 @@ __global__ __launch_bounds__(256) void moda_evict_move_kernel(EvictParams p, int
     }
 }
 
-// Longest cache whose keys stay in registers.
-constexpr int kEvInRegisters = 32 * kEvThreads;
-static size_t bit_words(int T) { return (size_t)((T + kEvThreads - 1) / kEvThreads) * kEvWaves; }
+// Longest cache that one workgroup chooses from.
+constexpr int kEvOneWorkgroup = 32 * kEvThreads;
 
 size_t evict_workspace_bytes(int B, int Hk, int T, int keep) {
-  if (T <= kEvInRegisters) return 16;
-  return (size_t)B * Hk * (bit_words(T) * sizeof(unsigned long long) + std::min(keep, T) * sizeof(int));
+  return T <= kEvOneWorkgroup ? 16 : evict_long_workspace_bytes((long long)B * Hk, T, std::min(keep, T));
 }
 
 hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t stream) {
@@ -257,17 +227,16 @@ hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t strea
   const int per_row_log2 = p.row_bytes == 128 ? 3 : p.row_bytes == 256 ? 4 : 5;  // pieces of 16 bytes of a row: 8, 16 or 32
   const long long chunks = (((long long)p.n << per_row_log2) + 256 * kMovePieces - 1) / (256 * kMovePieces);
   if (!grid_ok(groups, kEvThreads) || chunks > 0x7fffffff || !grid_ok(groups * chunks, 256)) return kGridTooLarge;
-  EvictScratch ws = {};
-  if (p.T > kEvInRegisters) {
-    ws.words = bit_words(p.T);
-    ws.bits = (unsigned long long*)workspace;
-    ws.list = (int*)(ws.bits + (size_t)groups * ws.words);
+  hipError_t e;
+  if (p.T > kEvOneWorkgroup) {
+    if (!evict_long_grid_ok(groups, p.T)) return kGridTooLarge;
+    e = launch_evict_choose_long(p, workspace, stream);
+  } else {
+    auto* choose = p.T <= 1 * kEvThreads ? moda_evict_choose_kernel<1> : p.T <= 2 * kEvThreads ? moda_evict_choose_kernel<2>
+                   : p.T <= 4 * kEvThreads ? moda_evict_choose_kernel<4> : p.T <= 8 * kEvThreads ? moda_evict_choose_kernel<8>
+                   : p.T <= 16 * kEvThreads ? moda_evict_choose_kernel<16> : moda_evict_choose_kernel<32>;
+    e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p);
   }
-  auto* choose = p.T <= 1 * kEvThreads ? moda_evict_choose_kernel<1> : p.T <= 2 * kEvThreads ? moda_evict_choose_kernel<2>
-                 : p.T <= 4 * kEvThreads ? moda_evict_choose_kernel<4> : p.T <= 8 * kEvThreads ? moda_evict_choose_kernel<8>
-                 : p.T <= 16 * kEvThreads ? moda_evict_choose_kernel<16> : p.T <= kEvInRegisters ? moda_evict_choose_kernel<32>
-                 : moda_evict_choose_kernel<0>;
-  const hipError_t e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p, ws);
   if (e != hipSuccess) return e;
   return launch_kernel(moda_evict_move_kernel, dim3((unsigned)(groups * chunks)), dim3(256), stream, p, per_row_log2, (int)chunks);
 }
