@@ -241,7 +241,8 @@ typedef struct {
  *   out: O [B, Hq, d], LSE [B, Hq] fp32; weights_out or NULL: weights_out[b,g,j] = weights_in[b,g,j] + the sum over
  *        the query heads h of group g of exp(logit of row j - LSE[b,h]), for the rows j of the own cache
  *   workspace: at least moda_attn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned; contents on entry
- *        are ignored.  `with_weights`: whether weights_out will be given.
+ *        are ignored.  `with_weights`: whether weights_out will be given.  The size never falls as s->T or prefix_rows
+ *        grows: what it is for the longest caches serves shorter ones.
  * A token that sees nothing (all lengths 0, no slots), or whose logits are all -inf, gets O = 0, LSE = -inf and
  * adds no weight.  s->causal is ignored.  bf16 only.  kv_alloc >= s->T >= 0.
  */

@@ -56,11 +56,10 @@ __device__ __forceinline__ int filled(const int* lengths, int i, int most) {
 // ---------------------------------------------------------------- rows on the vector ALUs
 // A lane owns 8 channels, d/8 lanes a row; a wave takes kU batches of 64 / (d/8) rows at a time, the next ones in
 // flight, and raises its reference once for them.  query(j) = the address of query j of GT (from nh on the last one repeats and is
-// not stored), `o_out`, `ml_out` = the first query's state, `scores` = the first one's logits of the first run, or null.
-template <int D, int GT, class Query>
-__device__ __forceinline__ void read_rows(const Rows& x, Query&& query, int nh, float c2, float* o_out,
-                                          float* ml_out, float* scores, size_t score_step, float* red) {
-  constexpr int LPR = D / 8, RPS = 64 / LPR, RB = D * 2, kU = 4, STEP = kShWaves * kU * RPS;
+// not stored), `scores` = the first one's logits of the first run, or null.  The waves' states go to red[wave][query][D + 2].
+template <int D, int GT, int WAVES, class Query>
+__device__ __forceinline__ void walk_rows(const Rows& x, Query&& query, int nh, float c2, float* scores, size_t score_step, float* red) {
+  constexpr int LPR = D / 8, RPS = 64 / LPR, RB = D * 2, kU = 4, STEP = WAVES * kU * RPS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = lane / LPR, l16 = lane % LPR;
   u32x4 q[GT];
   float m[GT], l[GT], o[GT][8];
@@ -149,22 +148,78 @@ __device__ __forceinline__ void read_rows(const Rows& x, Query&& query, int nh, 
 #pragma unroll
   for (int j = 0; j < GT; ++j) fold_groups<D>(m[j], l[j], o[j], c2, lane, red + (wave * GT + j) * (D + 2));
   __syncthreads();
-  for (int t = tid; t < GT * D; t += kShWaves * 64) {
-    const int j = t / D, ch = t % D;
-    if (j >= nh) continue;
-    float mm = -INFINITY, ll = 0.f, oo = 0.f;
+}
+
+// (reference, normaliser) of query j's waves, and channel ch's sum.
+template <int D, int GT, int WAVES>
+__device__ __forceinline__ f32x2 fold_rows(const float* red, int j, int ch, float c2, float& oo) {
+  float mm = -INFINITY, ll = 0.f;
+  oo = 0.f;
 #pragma unroll
-    for (int w = 0; w < kShWaves; ++w) mm = fmaxf(mm, red[(w * GT + j) * (D + 2) + D]);
+  for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, red[(w * GT + j) * (D + 2) + D]);
 #pragma unroll
-    for (int w = 0; w < kShWaves; ++w) {
-      const float* x = red + (w * GT + j) * (D + 2);
-      const float f = x[D] == -INFINITY ? 0.f : fast_exp2((x[D] - mm) * c2);
-      ll += f * x[D + 1];
-      oo += f * x[ch];
-    }
-    o_out[j * D + ch] = oo;
-    if (ch == 0) *(f32x2*)(ml_out + j * 2) = (f32x2){mm, ll};
+  for (int w = 0; w < WAVES; ++w) {
+    const float* x = red + (w * GT + j) * (D + 2);
+    const float f = x[D] == -INFINITY ? 0.f : fast_exp2((x[D] - mm) * c2);
+    ll += f * x[D + 1];
+    oo += f * x[ch];
   }
+  return (f32x2){mm, ll};
+}
+
+// ... and the queries' states to o_out, ml_out.
+template <int D, int GT, class Query>
+__device__ __forceinline__ void read_rows(const Rows& x, Query&& query, int nh, float c2, float* o_out, float* ml_out, float* scores,
+                                          size_t score_step, float* red) {
+  walk_rows<D, GT, kShWaves>(x, query, nh, c2, scores, score_step, red);
+  for (int t = threadIdx.x; t < nh * D; t += kShWaves * 64) {
+    const int j = t / D, ch = t % D;
+    float o;
+    const f32x2 ml = fold_rows<D, GT, kShWaves>(red, j, ch, c2, o);
+    o_out[t] = o;
+    if (ch == 0) *(f32x2*)(ml_out + j * 2) = ml;
+  }
+}
+
+// ---------------------------------------------------------------- short contexts: one kernel
+// No prefix, and as few rows as eight waves read in a few steps: a workgroup has all rows of a (batch, key/value head), GT heads at a
+// time, and finishes outputs and weights by itself; the logits stay in LDS.
+constexpr int kOneWaves = 8, kOneRows = 512;
+template <int D, int GT>
+__global__ __launch_bounds__(kOneWaves * 64, 2) void moda_shared_one_kernel(SharedParams p) {
+  constexpr int RB = D * 2;
+  __shared__ __attribute__((aligned(16))) float red[kOneWaves * GT * (D + 2)];
+  __shared__ float scores[GT][kOneRows], lse2[GT];
+  const int tid = threadIdx.x, G = p.Hq / p.Hk, b = blockIdx.x / p.Hk, g = blockIdx.x - b * p.Hk;
+  const float c2 = p.scale_log2;
+  const size_t at = (size_t)blockIdx.x * p.T_alloc * RB, slot_at = (size_t)blockIdx.x * p.depth_alloc * RB;
+  const int len = filled(p.lengths, b, p.T);
+  const Rows x = {(const char*)p.Ks + at, (const char*)p.Vs + at, len, (const char*)p.Kd + slot_at, (const char*)p.Vd + slot_at, p.depth_count};
+  static_assert(kOneRows <= kOneWaves * 64, "a thread per row");
+  float w = 0.f;
+  if (p.w_in && tid < len) w = p.w_in[(size_t)blockIdx.x * p.T_alloc + tid];
+  for (int h0 = 0; h0 < G; h0 += GT) {
+    const int nh = min(GT, G - h0);
+    const size_t bh = (size_t)b * p.Hq + g * G + h0;
+    if (h0 > 0) __syncthreads();  // (the heads before are done with LDS)
+    walk_rows<D, GT, kOneWaves>(x, [&](int j) { return (const char*)p.Q + (bh + j) * RB; }, nh, c2, p.w_out ? &scores[0][0] : nullptr, kOneRows, red);
+    for (int t = tid; t < nh * D; t += kOneWaves * 64) {
+      const int j = t / D, ch = t % D;
+      float o;
+      const f32x2 ml = fold_rows<D, GT, kOneWaves>(red, j, ch, c2, o);
+      const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
+      ((__bf16*)p.O)[(bh + j) * D + ch] = (__bf16)(none ? 0.f : o / ml[1]);
+      if (ch == 0) {
+        p.LSE[bh + j] = none ? -INFINITY : ml[0] * p.scale + __logf(ml[1]);
+        lse2[j] = none ? INFINITY : ml[0] * c2 + __log2f(ml[1]);
+      }
+    }
+    if (!p.w_out) continue;  // (uniform)
+    __syncthreads();
+    if (tid < len)
+      for (int j = 0; j < nh; ++j) w += fast_exp2(__builtin_fmaf(scores[j][tid], c2, -lse2[j]));
+  }
+  if (p.w_out && tid < len) p.w_out[(size_t)blockIdx.x * p.T_alloc + tid] = w;
 }
 
 // ---------------------------------------------------------------- rows on the matrix pipe
@@ -659,43 +714,85 @@ static int own_kind(int G) { return G > 4 ? 0 : G >= 3 ? 4 : G; }
 // Slices of a run of `rows` rows that `units` workgroups read each.  Long runs: `many` workgroups in all, which the chip holds at
 // once, as long as a slice has `good` rows; a second round of workgroups costs a workgroup's chain of latencies again, about
 // 5 us.  Runs that leave units without work: one workgroup per unit down to `least` rows, what the waves take at a time.
-static void cut(int rows, long long units, int many, int good, int least, int& n, int& per) {
+static long long slices_wanted(int rows, long long units, int many, int good, int least) {
   auto most = [&](int size) { return ((long long)rows + size - 1) / size; };
-  long long want = std::max(std::min(256 / units, most(least)), std::min(many / units, most(good)));
-  want = std::max(std::max(want, 1ll), ((long long)rows >> 22) + 1);  // (a slice is addressed with 32-bit byte offsets)
+  const long long want = std::max(std::min(256 / units, most(least)), std::min(many / units, most(good)));
+  return std::max(std::max(want, 1ll), ((long long)rows >> 22) + 1);  // (a slice is addressed with 32-bit byte offsets)
+}
+static void cut(int rows, long long units, int many, int good, int least, int& n, int& per) {
+  const long long want = slices_wanted(rows, units, many, good, least);
   per = (int)((rows + want - 1) / want + least - 1) / least * least;
   n = per > 0 ? (rows + per - 1) / per : 0;
 }
 
+// How the rows of prefixes and of own caches are cut.
+struct Cut {
+  long long units;
+  int many, good, least;
+};
+struct Plan {
+  int kind;        // SharedParams::prefix_kind
+  long long xg, cc;  // prefixes x key/value heads, column chunks of each
+  Cut prefix, own;
+  Plan(const SharedParams& p, int d) {
+    const int G = p.Hq / p.Hk, rows_at_once = kShWaves * 4 * 512 / d;  // (of read_rows)
+    const long long M = (long long)p.B / p.Np * G, groups = (long long)p.B * p.Hk;
+    kind = p.P == 0 ? 0 : M <= 4 ? 3 : M <= 32 ? 1 : M <= 64 ? 2 : 4;
+    xg = (long long)p.Np * p.Hk;
+    cc = kind == 2 || kind == 4 ? (M + kind * 32 - 1) / (kind * 32) : 1;
+    // By wave 256 workgroups: as many again come with the own rows (32 columns behind 32768 rows, 16 heads: 256 84.8 us, 768 93.8; 64
+    // heads of 2000 rows 19.5 / 25.8).  By workgroup 512, or 384 where own rows, a quarter of what the tiles walk or more, fill
+    // the rest (512 / 384: 512 columns behind 16384 rows, 64 x 500 own ones 51.1 / 48.3 us, 64 x 300 of d = 128 74.9 / 69.6; 128 behind
+    // 8192, 128 x 100 of d = 128 52.4 / 45.3; with one own row 512 behind 65536 110 / 124).
+    if (kind == 3) prefix = {xg, 512, 256, rows_at_once};
+    else if (kind <= 1) prefix = {xg, 256, 512, 128};
+    else prefix = {xg * cc, 4 * groups * p.T >= xg * cc * p.P ? 384 : 512, 256, 64};
+    if (own_kind(G) > 0) own = {groups, 512, 256, rows_at_once};
+    else own = {groups * ((G + 31) / 32), 512, 512, 128};
+  }
+};
+
 static void plan(SharedParams& p, int d) {
-  const int G = p.Hq / p.Hk;
-  const long long M = (long long)p.B / p.Np * G, xg = (long long)p.Np * p.Hk, groups = (long long)p.B * p.Hk;
-  p.prefix_kind = p.P == 0 ? 0 : M <= 4 ? 3 : M <= 32 ? 1 : M <= 64 ? 2 : 4;
+  const Plan l(p, d);
+  p.prefix_kind = l.kind;
   p.n_prefix = p.prefix_per = p.prefix_blocks = 0;
   if (p.P > 0) {
-    // (by wave: as many again come with the own rows.  32 columns behind 32768 rows, 16 heads: 256 workgroups 84.8 us, 768 93.8;
-    // 64 heads of 2000 rows 19.5 / 25.8)
-    const long long cc = (M + p.prefix_kind * 32 - 1) / (p.prefix_kind * 32);
-    if (p.prefix_kind == 3) cut(p.P, xg, 512, 256, kShWaves * 4 * 512 / d, p.n_prefix, p.prefix_per);
-    else if (p.prefix_kind == 1) cut(p.P, xg, 256, 512, 128, p.n_prefix, p.prefix_per);
-    else cut(p.P, xg * cc, 512, 256, 64, p.n_prefix, p.prefix_per);
-    const long long blocks = (xg * p.n_prefix + 7) / 8 * 8 * cc;
+    cut(p.P, l.prefix.units, l.prefix.many, l.prefix.good, l.prefix.least, p.n_prefix, p.prefix_per);
+    const long long blocks = (l.xg * p.n_prefix + 7) / 8 * 8 * l.cc;
     p.prefix_blocks = blocks > 0x7fffffff ? 0x7fffffff : (int)blocks;  // (too many: the launch is refused)
   }
-  if (own_kind(G) > 0) cut(p.T, groups, 512, 256, kShWaves * 4 * 512 / d, p.n_own, p.own_per);
-  else cut(p.T, groups * ((G + 31) / 32), 512, 512, 128, p.n_own, p.own_per);
+  cut(p.T, l.own.units, l.own.many, l.own.good, l.own.least, p.n_own, p.own_per);
   if (p.depth_count > 0) p.n_own = std::max(p.n_own, 1);
   p.n_slices = p.n_prefix + p.n_own;
   p.score_step = ((size_t)p.T + 31) / 32 * 32;
 }
 
-static size_t states(const SharedParams& p) { return ((size_t)p.B * p.Hq * p.n_slices + 1) / 2 * 2; }  // (even: 16-byte pieces)
+// Calls that take one kernel: no prefix, and few steps of rows (128 at d = 128, 256 at d = 64), more of them where the workgroups fill
+// half the chip anyway; groups of more than 4 heads, in turns of 4, one step and d = 128.  Two kernels / one, us, (batch x
+// key/value heads), rows, with weights:
+//   1 head   d=64 16, 20 7.1 / 4.7;   64, 500 7.2 / 5.4;   512, 500 13.8 / 9.8;   d=128 16, 250 7.8 / 6.7;   16, 500 7.2 / 7.6;   512, 500 23.0 / 18.5
+//   2 heads  d=64 8, 500 7.5 / 6.5;   d=128 8, 120 7.3 / 4.9;   8, 250 8.1 / 7.5;   8, 500 7.5 / 8.9;   256, 500 14.7 / 10.5
+//   4 heads  d=64 8, 250 9.6 / 8.5;   8, 500 8.5 / 8.7;   d=128 8, 120 8.5 / 6.3;   8, 250 9.8 / 10.3;   8, 500 8.8 / 12.5;   256, 500 19.7 / 14.2
+//   8 heads  d=64 8, 120 10.6 / 10.5;   256, 250 13.5 / 15.2;   d=128 8, 120 12.3 / 10.3;   8, 250 12.6 / 18.6;   256, 250 15.6 / 20.2
+static bool in_one(const SharedParams& p, int d) {
+  if (p.P > 0 || p.T > kOneRows) return false;
+  const int G = p.Hq / p.Hk, step = kOneWaves * 4 * 512 / d;
+  const long long steps = ((long long)p.T + p.depth_count + step - 1) / step;
+  if (G > 4) return G <= 8 && d == 128 && steps <= 1;
+  if ((long long)p.B * p.Hk >= 128) return steps <= 4;
+  return steps <= (G == 1 ? 4 : G == 2 || d == 64 ? 2 : 1);
+}
 
+static size_t state_count(const SharedParams& p) { return ((size_t)p.B * p.Hq * p.n_slices + 1) / 2 * 2; }  // (even: 16-byte pieces)
+
+// What every shorter own cache and prefix takes at most: cuts have no more slices than are wanted, and those never get fewer.
 size_t decode_shared_workspace_bytes(const SharedParams& dims, int d, bool with_weights) {
   SharedParams p = dims;
   plan(p, d);
-  const size_t bytes = (states(p) * (d + 2) + (with_weights ? (size_t)p.B * p.Hq * p.score_step : 0)) * sizeof(float);
-  return std::max<size_t>(bytes, 16);
+  const Plan l(p, d);
+  const long long own = p.T > 0 ? slices_wanted(p.T, l.own.units, l.own.many, l.own.good, l.own.least) : 0;
+  p.n_slices = (int)(std::max(own, 1ll) + (p.P > 0 ? slices_wanted(p.P, l.prefix.units, std::max(l.prefix.many, l.kind > 1 ? 512 : 0), l.prefix.good, l.prefix.least) : 0));
+  return (state_count(p) * (d + 2) + (with_weights ? (size_t)p.B * p.Hq * p.score_step : 0)) * sizeof(float);
 }
 
 template <int D, int PREFIX>
@@ -709,6 +806,12 @@ static void (*slices_kernel(int own))(SharedParams) {
 template <int D>
 static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
   const int G = p.Hq / p.Hk, own = own_kind(G);
+  if (in_one(p, D)) {
+    const long long groups = (long long)p.B * p.Hk;
+    if (!grid_ok(groups, kOneWaves * 64)) return kGridTooLarge;
+    return launch_kernel(G >= 3 ? moda_shared_one_kernel<D, 4> : G == 2 ? moda_shared_one_kernel<D, 2> : moda_shared_one_kernel<D, 1>,
+                         dim3((unsigned)groups), dim3(kOneWaves * 64), stream, p);
+  }
   const int heads_per = own > 0 ? own : 32;
   const long long blocks = p.prefix_blocks + (long long)p.B * p.Hk * ((G + heads_per - 1) / heads_per) * p.n_own;
   // teams of a workgroup that share a head's slices, so that each folds four or fewer of them at a time
@@ -731,8 +834,8 @@ static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
 hipError_t launch_decode_shared(SharedParams p, int d, void* workspace, hipStream_t stream) {
   plan(p, d);
   p.ws_o = (float*)workspace;
-  p.ws_ml = p.ws_o + states(p) * d;
-  p.scores = p.ws_ml + states(p) * 2;
+  p.ws_ml = p.ws_o + state_count(p) * d;
+  p.scores = p.ws_ml + state_count(p) * 2;
   return d == 128 ? launch_d<128>(p, stream) : launch_d<64>(p, stream);
 }
 

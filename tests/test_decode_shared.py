@@ -252,9 +252,9 @@ def test_captured_calls_and_streams():
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g, stream=side):
             call()
-        graphs.append((g, x, lens, w_in, w, out, lse))
+        graphs.append((g, x, lens, w_in, w, out, lse, ws))  # (everything that the graph reads or writes has to live as long)
     for step in range(3):
-        for g, x, lens, w_in, w, out, lse in graphs:
+        for g, x, lens, w_in, w, out, lse, _ in graphs:
             x["Q"].copy_(torch.randn_like(x["Q"]))
             lens.copy_(ints([300 - step, 20 + step, step, 150]))
             w.zero_()
@@ -266,7 +266,7 @@ def test_captured_calls_and_streams():
             assert torch.equal(O, out) and torch.equal(LSE, lse) and torch.equal(w, w2)
     with torch.cuda.stream(side):
         side.wait_stream(torch.cuda.default_stream())
-        _, x, lens, w_in, w, out, lse = graphs[0]
+        _, x, lens, w_in, w, out, lse, _ = graphs[0]
         O, LSE = moda_attn_decode_shared(**x, lengths=lens)
     side.synchronize()
     assert torch.equal(O, out) and torch.equal(LSE, lse)
@@ -309,6 +309,25 @@ def test_refusals_without_gpu():
     p = ctypes.c_void_p(0x1000)
     weights = lambda w, T=16: lib().moda_attn_decode_weights(p, p, p, p, p, p, p, w, p, p, T, p, 1, ctypes.byref(MODAShape(**OK)), None)
     assert weights(None) == 1 and weights(p) == 6 and weights(p, 15) == 2
+
+
+@pytest.mark.parametrize("B,Hq,Hk,d,Np", [(1, 16, 16, 128, 1), (4, 16, 16, 64, 1), (8, 64, 8, 64, 2), (64, 64, 8, 128, 1), (40, 8, 8, 128, 1),
+                                          (96, 32, 8, 64, 3), (600, 8, 1, 128, 600)])
+def test_workspace_of_the_longest_caches_serves_shorter_ones(B, Hq, Hk, d, Np):
+    from paper_2603_15619_amd.binding import MODAPrefix, MODAShape, lib
+
+    def need(T, P, w):
+        return lib().moda_attn_decode_shared_workspace_bytes(ctypes.byref(MODAPrefix(Np, P, P)), w,
+                                                             ctypes.byref(MODAShape(B, Hq, Hk, T, d, 4, 4, 1, 0.0, 1)))
+
+    sizes = [*range(0, 3000, 7), *range(3000, 70000, 531)]
+    for w in (0, 1):
+        for P in (0, 100, 5000, 40000):
+            row = [need(T, P, w) for T in sizes]
+            assert all(a <= b for a, b in zip(row, row[1:])), (P, w)
+        for T in (0, 100, 5000):
+            row = [need(T, P, w) for P in sizes]
+            assert all(a <= b for a, b in zip(row, row[1:])), (T, w)
 
 
 def test_binding_refusals_without_gpu():
