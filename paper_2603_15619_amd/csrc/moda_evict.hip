@@ -13,28 +13,29 @@
 
 namespace moda {
 
-constexpr int kEvThreads = 1024, kEvWaves = kEvThreads / 64;
+constexpr int kEvThreads = 1024;  // most threads of the workgroup that chooses
 
+// THREADS: few for few rows, whose barriers and sums over the waves are then shorter.
 // Rows of a (sequence, head): wave w takes N times 64 of them, from w * N * 64 on; a row's key stays in a register from its one
 // read on.
-template <int N>
-__global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictParams p) {
-  constexpr int kBins = 2048;
+template <int N, int THREADS>
+__global__ __launch_bounds__(THREADS) void moda_evict_choose_kernel(EvictParams p) {
+  constexpr int kBins = 2048, kWaves = THREADS / 64, kPer = kBins / THREADS;
   __shared__ unsigned hist[kBins];
-  __shared__ int part[kEvWaves], part2[kEvWaves];
+  __shared__ int part[kWaves], part2[kWaves];
   __shared__ unsigned s_digit;
   __shared__ int s_need;
   // rows that stay, a bit each; rows that move, in ascending order (half of all at most: as many as there are holes)
-  __shared__ unsigned long long bits[kEvWaves * N];
-  __shared__ unsigned short list[kEvThreads * N / 2];
+  __shared__ unsigned long long bits[kWaves * N];
+  __shared__ unsigned short list[THREADS * N / 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int bg = blockIdx.x, b = bg / p.Hk;
   const int len = p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
   const int fit = min(len, p.keep);
   int* index = p.index + (size_t)bg * p.n;
-  for (int r = fit + tid; r < p.n; r += kEvThreads) index[r] = -1;
+  for (int r = fit + tid; r < p.n; r += THREADS) index[r] = -1;
   if (len <= p.keep) {
-    for (int r = tid; r < fit; r += kEvThreads) index[r] = r;
+    for (int r = tid; r < fit; r += THREADS) index[r] = r;
     return;
   }
   const float* w = p.w + (size_t)bg * p.T_alloc;
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
       if (lane == 0) part[wave] = newest;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kEvWaves; ++i) newest = max(newest, part[i]);
+      for (int i = 0; i < kWaves; ++i) newest = max(newest, part[i]);
       __syncthreads();
     }
     above = (long long)newest - p.recent;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
   int need = fit;
   auto digit = [&](int shift) {
     const unsigned mask = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
-    for (int i = tid; i < kBins; i += kEvThreads) hist[i] = 0;
+    for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
     __syncthreads();
     each([&](int i) {
       const unsigned k = keys[i];
@@ -97,8 +98,10 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
       }
     });
     __syncthreads();
-    // thread t: bins 2047 - 2 t and 2046 - 2 t; `sum` = rows in the bins of threads up to this one
-    const int hi = (int)hist[kBins - 1 - 2 * tid], both = hi + (int)hist[kBins - 2 - 2 * tid];
+    // thread t: kPer bins from kBins - 1 - kPer t down; `sum` = rows in the bins of threads up to this one
+    int c[kPer], both = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) both += c[i] = (int)hist[kBins - 1 - kPer * tid - i];
     int sum = both;
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
@@ -108,11 +111,17 @@ __global__ __launch_bounds__(kEvThreads) void moda_evict_choose_kernel(EvictPara
     if (lane == 63) part[wave] = sum;
     __syncthreads();
     for (int i = 0; i < wave; ++i) sum += part[i];
-    const int before = sum - both;
+    int before = sum - both;
     if (before < need && sum >= need) {  // (one thread)
-      const bool first = need - before <= hi;
-      s_digit = kBins - 1 - 2 * tid - (first ? 0 : 1);
-      s_need = need - before - (first ? 0 : hi);
+      int i = 0;
+#pragma unroll
+      for (int x = 0; x < kPer - 1; ++x)
+        if (i == x && before + c[x] < need) {
+          before += c[x];
+          ++i;
+        }
+      s_digit = kBins - 1 - kPer * tid - i;
+      s_need = need - before;
     }
     __syncthreads();
     threshold |= s_digit << shift;
@@ -232,10 +241,13 @@ hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t strea
     if (!evict_long_grid_ok(groups, p.T)) return kGridTooLarge;
     e = launch_evict_choose_long(p, workspace, stream);
   } else {
-    auto* choose = p.T <= 1 * kEvThreads ? moda_evict_choose_kernel<1> : p.T <= 2 * kEvThreads ? moda_evict_choose_kernel<2>
-                   : p.T <= 4 * kEvThreads ? moda_evict_choose_kernel<4> : p.T <= 8 * kEvThreads ? moda_evict_choose_kernel<8>
-                   : p.T <= 16 * kEvThreads ? moda_evict_choose_kernel<16> : moda_evict_choose_kernel<32>;
-    e = launch_kernel(choose, dim3((unsigned)groups), dim3(kEvThreads), stream, p);
+    // (1024 / 256 threads, 8 heads, half of the rows stay, whole call: T=100 10.6 / 9.7 us, T=500 10.9 / 10.9, T=1090 12.2 / 15.0)
+    const int threads = p.T <= 512 ? 256 : kEvThreads;
+    auto* choose = p.T <= 512 ? moda_evict_choose_kernel<2, 256> : p.T <= 1024 ? moda_evict_choose_kernel<1, 1024>
+                   : p.T <= 2048 ? moda_evict_choose_kernel<2, 1024> : p.T <= 4096 ? moda_evict_choose_kernel<4, 1024>
+                   : p.T <= 8192 ? moda_evict_choose_kernel<8, 1024> : p.T <= 16384 ? moda_evict_choose_kernel<16, 1024>
+                   : moda_evict_choose_kernel<32, 1024>;
+    e = launch_kernel(choose, dim3((unsigned)groups), dim3(threads), stream, p);
   }
   if (e != hipSuccess) return e;
   return launch_kernel(moda_evict_move_kernel, dim3((unsigned)(groups * chunks)), dim3(256), stream, p, per_row_log2, (int)chunks);

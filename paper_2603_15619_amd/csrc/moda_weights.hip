@@ -67,8 +67,7 @@ __global__ __launch_bounds__(kWfWaves * 64, 2) void moda_weights_f32_kernel(Weig
   float acc[16], x = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-  auto load = [&](int u) {  // (units past the end repeat the last one)
-    u = min(u, u1 - 1);
+  auto load = [&](int u) {
     const size_t row = ((size_t)b * p.Hq + g * G + u / nq) * p.T + min(t0 + u % nq * 32 + l32, len - 1);
     next.load((const float*)p.Q + row * D, hi);
     x = p.LSE[row];
@@ -79,7 +78,7 @@ __global__ __launch_bounds__(kWfWaves * 64, 2) void moda_weights_f32_kernel(Weig
     const RowF32<D> qf = next;
     // a query that sees nothing has LSE -inf and logits -inf
     const float lse2 = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
-    load(u + kWfWaves);
+    if (u + kWfWaves < u1) load(u + kWfWaves);  // (uniform)
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
