@@ -12,7 +12,7 @@
 //   prefixes   all queries that share a prefix (sequences x heads of a group) are the columns of matrix products
 //              S^T = K Q^T, O^T += V^T P^T; up to 4 take the vector ALUs (read_rows).  Up to 32 (read_by_wave): every wave reads its own part of the slice.
 //              More (read_by_workgroup): 2 or 4 waves of 32 columns share the K and V tiles of a slice in LDS.
-//   own rows   up to 4 heads per group on the vector ALUs (read_rows), more as the columns of read_by_wave.
+//   own rows   up to 2 heads per group on the vector ALUs (read_rows), more as the columns of read_by_wave.
 #include <algorithm>
 
 #include "moda_decode_fold.h"
@@ -481,7 +481,7 @@ __device__ __forceinline__ void read_by_workgroup(Columns<D>& c, bool idle, cons
 
 // ---------------------------------------------------------------- all slices
 // PREFIX: how prefixes are read (0: none, 1: by wave, 2 / 4: by workgroup, so many waves of columns, 3: vector ALUs).  OWN: heads per
-// workgroup on the vector ALUs (1, 2, 4), or 0: by wave on the matrix pipe.
+// workgroup on the vector ALUs (1, 2), or 0: by wave on the matrix pipe.
 template <int D, int PREFIX, int OWN>
 constexpr int slices_lds() {
   // the ring; or 32 rows of K and V of each wave, where their states go afterwards; or the waves' states of OWN heads
@@ -709,7 +709,8 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
 }
 
 // ---------------------------------------------------------------- the cut into slices
-static int own_kind(int G) { return G > 4 ? 0 : G >= 3 ? 4 : G; }
+// (3 and 4 heads: 16 x 3000 rows, 32 heads on 8, d = 128, with weights, vector ALUs 42.4 us, matrix pipe 36.0; 64 x 700 40.3 / 36.5)
+static int own_kind(int G) { return G > 2 ? 0 : G; }
 
 // Slices of a run of `rows` rows that `units` workgroups read each.  Long runs: `many` workgroups in all, which the chip holds at
 // once, as long as a slice has `good` rows; a second round of workgroups costs a workgroup's chain of latencies again, about
@@ -747,7 +748,9 @@ struct Plan {
     if (kind == 3) prefix = {xg, 512, 256, rows_at_once};
     else if (kind <= 1) prefix = {xg, 256, 512, 128};
     else prefix = {xg * cc, 4 * groups * p.T >= xg * cc * p.P ? 384 : 512, 256, 64};
-    if (own_kind(G) > 0) own = {groups, 512, 256, rows_at_once};
+    // Beside prefixes, whose workgroups last longer, more of the long own caches' (16 x 2000 rows behind 16000, 16 heads of d = 128, 512 /
+    // 1024: 63.5 / 57.1 us; without a prefix 16 x 2000 38.5 / 39.4).
+    if (own_kind(G) > 0) own = p.P > 0 ? Cut{groups, 1024, 512, rows_at_once} : Cut{groups, 512, 256, rows_at_once};
     else own = {groups * ((G + 31) / 32), 512, 512, 128};
   }
 };
@@ -790,17 +793,19 @@ size_t decode_shared_workspace_bytes(const SharedParams& dims, int d, bool with_
   SharedParams p = dims;
   plan(p, d);
   const Plan l(p, d);
-  const long long own = p.T > 0 ? slices_wanted(p.T, l.own.units, l.own.many, l.own.good, l.own.least) : 0;
+  long long own = p.T > 0 ? slices_wanted(p.T, l.own.units, l.own.many, l.own.good, l.own.least) : 0;
+  SharedParams alone = dims;  // (the same without a prefix)
+  alone.P = 0;
+  const Plan a(alone, d);
+  if (p.T > 0) own = std::max(own, slices_wanted(p.T, a.own.units, a.own.many, a.own.good, a.own.least));
   p.n_slices = (int)(std::max(own, 1ll) + (p.P > 0 ? slices_wanted(p.P, l.prefix.units, std::max(l.prefix.many, l.kind > 1 ? 512 : 0), l.prefix.good, l.prefix.least) : 0));
   return (state_count(p) * (d + 2) + (with_weights ? (size_t)p.B * p.Hq * p.score_step : 0)) * sizeof(float);
 }
 
 template <int D, int PREFIX>
 static void (*slices_kernel(int own))(SharedParams) {
-  if constexpr (PREFIX == 3)  // (4 queries at most: so are the heads of a group)
-    return own == 4 ? moda_shared_slices_kernel<D, 3, 4> : own == 2 ? moda_shared_slices_kernel<D, 3, 2> : moda_shared_slices_kernel<D, 3, 1>;
-  else return own == 4 ? moda_shared_slices_kernel<D, PREFIX, 4> : own == 2 ? moda_shared_slices_kernel<D, PREFIX, 2>
-         : own == 1 ? moda_shared_slices_kernel<D, PREFIX, 1> : moda_shared_slices_kernel<D, PREFIX, 0>;
+  return own == 2 ? moda_shared_slices_kernel<D, PREFIX, 2> : own == 1 ? moda_shared_slices_kernel<D, PREFIX, 1>
+                                                                       : moda_shared_slices_kernel<D, PREFIX, 0>;
 }
 
 template <int D>

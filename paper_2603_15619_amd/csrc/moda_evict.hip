@@ -241,7 +241,7 @@ hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t strea
     if (!evict_long_grid_ok(groups, p.T)) return kGridTooLarge;
     e = launch_evict_choose_long(p, workspace, stream);
   } else {
-    // (1024 / 256 threads, 8 heads, half of the rows stay, whole call: T=100 10.6 / 9.7 us, T=500 10.9 / 10.9, T=1090 12.2 / 15.0)
+    // (1024 / 256 threads, 8 heads, half of the rows stay, whole call: T=100 10.6 / 9.0 us, T=500 10.9 / 9.4, T=1090 12.2 / 15.0)
     const int threads = p.T <= 512 ? 256 : kEvThreads;
     auto* choose = p.T <= 512 ? moda_evict_choose_kernel<2, 256> : p.T <= 1024 ? moda_evict_choose_kernel<1, 1024>
                    : p.T <= 2048 ? moda_evict_choose_kernel<2, 1024> : p.T <= 4096 ? moda_evict_choose_kernel<4, 1024>

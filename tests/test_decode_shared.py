@@ -114,6 +114,13 @@ SHAPES = [
     dict(B=2, Hq=80, Hk=2, T=100, d=128, L=70, P=65),
     dict(B=17, Hq=16, Hk=2, T=0, d=64, L=0, P=700, Np=17),
     dict(B=40, Hq=16, Hk=2, T=20, d=128, L=4, P=96),
+    # two to four queries per prefix and head; 33 to 64 of them
+    dict(B=2, Hq=8, Hk=2, T=40, d=128, L=2, P=300, Np=2),
+    dict(B=2, Hq=3, Hk=1, T=600, d=64, L=0, P=150, Np=2),
+    dict(B=2, Hq=4, Hk=2, T=0, d=64, L=5, P=70),
+    dict(B=8, Hq=8, Hk=1, T=20, d=128, L=3, P=500),
+    dict(B=12, Hq=4, Hk=1, T=300, d=64, L=0, P=1100),
+    dict(B=35, Hq=2, Hk=2, T=65, d=128, L=1, P=63),
 ]
 
 
@@ -131,6 +138,16 @@ def test_shared_prefix(c):
     (7, 16, 2, 257, 64, 64, [256, 255, 257, 31, 32, 33, 0]), (2, 3, 1, 600, 64, 1, None), (2, 2, 1, 65, 128, 0, [65, 64])])
 def test_ragged_lengths_and_weights(B, Hq, Hk, T, d, L, lens):
     check(B, Hq, Hk, T, d, L, lens=lens, kv_alloc=T + 5, seed=T + L)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,Hq,Hk,T,d,L,lens", [
+    (3, 10, 2, 100, 128, 4, [100, 0, 33]), (2, 8, 1, 121, 128, 7, [121, 1]), (2, 7, 1, 128, 128, 0, [128, 127]), (3, 8, 2, 300, 64, 5, [300, 299, 2]),
+    (64, 4, 2, 512, 64, 1, None), (64, 2, 2, 511, 128, 0, None), (1, 1, 1, 1, 128, 0, [0]), (2, 4, 4, 0, 64, 9, None), (5, 6, 3, 255, 64, 1, [255, 256, 0, 64, 65]),
+    (50, 12, 3, 400, 128, 2, None)])
+def test_short_contexts(B, Hq, Hk, T, d, L, lens):
+    check(B, Hq, Hk, T, d, L, lens=lens, kv_alloc=T + 3, seed=T)
+    check(B, Hq, Hk, T, d, L, lens=lens, kv_alloc=T + 1, seed=T + 1, weights=False)
 
 
 @pytest.mark.gpu
