@@ -195,7 +195,7 @@ const char* moda_status_string(moda_status st) {
   return "unknown status";
 }
 
-int moda_version(void) { return 200; }
+int moda_version(void) { return 300; }
 
 int moda_kernels_per_call(const moda_shape* s, int which) {
   if (check_shape(s) != MODA_OK || s->B == 0 || s->T == 0) return 0;

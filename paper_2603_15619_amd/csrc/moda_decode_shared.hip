@@ -9,10 +9,13 @@
 // there too (4 bytes per row and head, where a row of K and V is 4 d bytes), since no slice knows the LSE.
 //
 // One launch takes all slices:
-//   prefixes   all queries that share a prefix (sequences x heads of a group) are the columns of matrix products
-//              S^T = K Q^T, O^T += V^T P^T; up to 4 take the vector ALUs (read_rows).  Up to 32 (read_by_wave): every wave reads its own part of the slice.
-//              More (read_by_workgroup): 2 or 4 waves of 32 columns share the K and V tiles of a slice in LDS.
+//   prefixes   all queries that share a prefix (sequences x heads of a group) read its rows together.  Up to 4 of them on the vector
+//              ALUs (read_rows), else they are the columns of matrix products S^T = K Q^T, O^T += V^T P^T: up to 32
+//              (read_by_wave) every wave reads its own part of the slice; more (read_by_workgroup), 2 or 4 waves of 32 columns
+//              share the K and V tiles of the slice in LDS.
 //   own rows   up to 2 heads per group on the vector ALUs (read_rows), more as the columns of read_by_wave.
+// What bounds it: long calls the reads (32 sequences behind 32768 rows 5.6 TB/s; 8 x 65536 own rows with weights 5.7), 512 queries per
+// prefix row the vector ALUs (exponentials; 720 TFLOP/s at 65536 rows, d = 128), short ones two launches of about 4 us.
 #include <algorithm>
 
 #include "moda_decode_fold.h"
