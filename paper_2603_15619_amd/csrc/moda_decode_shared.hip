@@ -13,7 +13,8 @@
 //              ALUs (read_rows), else they are the columns of matrix products S^T = K Q^T, O^T += V^T P^T: up to 32
 //              (read_by_wave) every wave reads its own part of the slice; more (read_by_workgroup), 2 or 4 waves of 32 columns
 //              share the K and V tiles of the slice in LDS.
-//   own rows   up to 2 heads per group on the vector ALUs (read_rows), more as the columns of read_by_wave.
+//   own rows   up to 2 heads per group on the vector ALUs (read_rows), where all caches are short up to 8 (own_kind), else the heads
+//              are the columns of read_by_wave.
 // What bounds it: long calls the reads (32 sequences behind 32768 rows 5.6 TB/s; 8 x 65536 own rows with weights 5.7), 512 queries per
 // prefix row the vector ALUs (exponentials; 720 TFLOP/s at 65536 rows, d = 128), short ones two launches of about 4 us.
 #include <algorithm>
@@ -185,8 +186,8 @@ __device__ __forceinline__ void read_rows(const Rows& x, Query&& query, int nh, 
 }
 
 // ---------------------------------------------------------------- short contexts: one kernel
-// No prefix, and as few rows as eight waves read in a few steps: a workgroup has all rows of a (batch, key/value head), GT heads at a
-// time, and finishes outputs and weights by itself; the logits stay in LDS.
+// No prefix, up to 4 heads per group, and as few rows as eight waves read in a few steps: a workgroup has all rows of a (batch,
+// key/value head) and finishes outputs and weights by itself; the logits stay in LDS.
 constexpr int kOneWaves = 8, kOneRows = 512;
 template <int D, int GT>
 __global__ __launch_bounds__(kOneWaves * 64, 2) void moda_shared_one_kernel(SharedParams p) {
@@ -201,28 +202,25 @@ __global__ __launch_bounds__(kOneWaves * 64, 2) void moda_shared_one_kernel(Shar
   static_assert(kOneRows <= kOneWaves * 64, "a thread per row");
   float w = 0.f;
   if (p.w_in && tid < len) w = p.w_in[(size_t)blockIdx.x * p.T_alloc + tid];
-  for (int h0 = 0; h0 < G; h0 += GT) {
-    const int nh = min(GT, G - h0);
-    const size_t bh = (size_t)b * p.Hq + g * G + h0;
-    if (h0 > 0) __syncthreads();  // (the heads before are done with LDS)
-    walk_rows<D, GT, kOneWaves>(x, [&](int j) { return (const char*)p.Q + (bh + j) * RB; }, nh, c2, p.w_out ? &scores[0][0] : nullptr, kOneRows, red);
-    for (int t = tid; t < nh * D; t += kOneWaves * 64) {
-      const int j = t / D, ch = t % D;
-      float o;
-      const f32x2 ml = fold_rows<D, GT, kOneWaves>(red, j, ch, c2, o);
-      const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
-      ((__bf16*)p.O)[(bh + j) * D + ch] = (__bf16)(none ? 0.f : o / ml[1]);
-      if (ch == 0) {
-        p.LSE[bh + j] = none ? -INFINITY : ml[0] * p.scale + __logf(ml[1]);
-        lse2[j] = none ? INFINITY : ml[0] * c2 + __log2f(ml[1]);
-      }
+  const size_t bh = (size_t)b * p.Hq + g * G;
+  walk_rows<D, GT, kOneWaves>(x, [&](int j) { return (const char*)p.Q + (bh + j) * RB; }, G, c2, p.w_out ? &scores[0][0] : nullptr, kOneRows, red);
+  for (int t = tid; t < G * D; t += kOneWaves * 64) {
+    const int j = t / D, ch = t % D;
+    float o;
+    const f32x2 ml = fold_rows<D, GT, kOneWaves>(red, j, ch, c2, o);
+    const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
+    ((__bf16*)p.O)[(bh + j) * D + ch] = (__bf16)(none ? 0.f : o / ml[1]);
+    if (ch == 0) {
+      p.LSE[bh + j] = none ? -INFINITY : ml[0] * p.scale + __logf(ml[1]);
+      lse2[j] = none ? INFINITY : ml[0] * c2 + __log2f(ml[1]);
     }
-    if (!p.w_out) continue;  // (uniform)
-    __syncthreads();
-    if (tid < len)
-      for (int j = 0; j < nh; ++j) w += fast_exp2(__builtin_fmaf(scores[j][tid], c2, -lse2[j]));
   }
-  if (p.w_out && tid < len) p.w_out[(size_t)blockIdx.x * p.T_alloc + tid] = w;
+  if (!p.w_out) return;  // (uniform)
+  __syncthreads();
+  if (tid < len) {
+    for (int j = 0; j < G; ++j) w += fast_exp2(__builtin_fmaf(scores[j][tid], c2, -lse2[j]));
+    p.w_out[(size_t)blockIdx.x * p.T_alloc + tid] = w;
+  }
 }
 
 // ---------------------------------------------------------------- rows on the matrix pipe
@@ -484,7 +482,7 @@ __device__ __forceinline__ void read_by_workgroup(Columns<D>& c, bool idle, cons
 
 // ---------------------------------------------------------------- all slices
 // PREFIX: how prefixes are read (0: none, 1: by wave, 2 / 4: by workgroup, so many waves of columns, 3: vector ALUs).  OWN: heads per
-// workgroup on the vector ALUs (1, 2), or 0: by wave on the matrix pipe.
+// workgroup on the vector ALUs (1, 2, 4), or 0: by wave on the matrix pipe.
 template <int D, int PREFIX, int OWN>
 constexpr int slices_lds() {
   // the ring; or 32 rows of K and V of each wave, where their states go afterwards; or the waves' states of OWN heads
@@ -712,8 +710,17 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
 }
 
 // ---------------------------------------------------------------- the cut into slices
-// (3 and 4 heads: 16 x 3000 rows, 32 heads on 8, d = 128, with weights, vector ALUs 42.4 us, matrix pipe 36.0; 64 x 700 40.3 / 36.5)
-static int own_kind(int G) { return G > 2 ? 0 : G; }
+// How own rows are read: 0 on the matrix pipe, else heads per workgroup on the vector ALUs.  A workgroup of the latter is through in
+// half the time, one of the former does less per row: from 3 heads on by the rows of all caches (vector ALUs / matrix pipe, us, with
+// weights, 4 heads a group, (batch x key/value heads), rows):
+//   d=64   8, 600 8.4 / 10.1;   8, 5000 10.5 / 12.5;   32, 1200 10.1 / 12.0;   32, 2500 12.9 / 13.1;   8, 12000 14.0 / 13.8;   128, 5000 37.8 / 36.0
+//   d=128  8, 600 8.6 / 11.9;   8, 5000 12.6 / 14.7;   32, 1200 11.9 / 14.5;   32, 2500 18.1 / 15.9;   8, 12000 20.3 / 16.8;   512, 2500 127 / 120
+//   8 heads, in two workgroups:  d=64 8, 1200 8.9 / 10.4;   8, 2500 10.4 / 11.0;   8, 5000 13.3 / 12.6;   d=128 8, 1200 10.9 / 12.4;   8, 5000 19.0 / 14.8
+static int own_kind(const SharedParams& p) {
+  const int G = p.Hq / p.Hk;
+  if (G <= 2) return G;
+  return G <= 8 && (long long)p.B * p.Hk * p.T < (G <= 4 ? 65536 : 24576) ? 4 : 0;
+}
 
 // Slices of a run of `rows` rows that `units` workgroups read each.  Long runs: `many` workgroups in all, which the chip holds at
 // once, as long as a slice has `good` rows; a second round of workgroups costs a workgroup's chain of latencies again, about
@@ -735,7 +742,7 @@ struct Cut {
   int many, good, least;
 };
 struct Plan {
-  int kind;        // SharedParams::prefix_kind
+  int kind, own_heads;  // SharedParams::prefix_kind, own_kind
   long long xg, cc;  // prefixes x key/value heads, column chunks of each
   Cut prefix, own;
   Plan(const SharedParams& p, int d) {
@@ -753,8 +760,13 @@ struct Plan {
     else prefix = {xg * cc, 4 * groups * p.T >= xg * cc * p.P ? 384 : 512, 256, 64};
     // Beside prefixes, whose workgroups last longer, more of the long own caches' (16 x 2000 rows behind 16000, 16 heads of d = 128, 512 /
     // 1024: 63.5 / 57.1 us; without a prefix 16 x 2000 38.5 / 39.4).
-    if (own_kind(G) > 0) own = p.P > 0 ? Cut{groups, 1024, 512, rows_at_once} : Cut{groups, 512, 256, rows_at_once};
-    else own = {groups * ((G + 31) / 32), 512, 512, 128};
+    own_heads = own_kind(p);
+    own = own_cut(groups, G, own_heads, p.P > 0, rows_at_once);
+  }
+  static Cut own_cut(long long groups, int G, int heads, bool prefix, int rows_at_once) {
+    if (heads == 0) return {groups * ((G + 31) / 32), 512, 512, 128};
+    const long long units = groups * ((G + heads - 1) / heads);
+    return prefix ? Cut{units, 1024, 512, rows_at_once} : Cut{units, 512, 256, rows_at_once};
   }
 };
 
@@ -773,20 +785,16 @@ static void plan(SharedParams& p, int d) {
   p.score_step = ((size_t)p.T + 31) / 32 * 32;
 }
 
-// Calls that take one kernel: no prefix, and few steps of rows (128 at d = 128, 256 at d = 64), more of them where the workgroups fill
-// half the chip anyway; groups of more than 4 heads, in turns of 4, one step and d = 128.  Two kernels / one, us, (batch x
-// key/value heads), rows, with weights:
+// Calls that take one kernel: no prefix, up to 4 heads per group, and few steps of rows (128 at d = 128, 256 at d = 64), more of them
+// where the workgroups fill half the chip anyway.  Two kernels / one, us, (batch x key/value heads), rows, with weights:
 //   1 head   d=64 16, 20 7.1 / 4.7;   64, 500 7.2 / 5.4;   512, 500 13.8 / 9.8;   d=128 16, 250 7.8 / 6.7;   16, 500 7.2 / 7.6;   512, 500 23.0 / 18.5
 //   2 heads  d=64 8, 500 7.5 / 6.5;   d=128 8, 120 7.3 / 4.9;   8, 250 8.1 / 7.5;   8, 500 7.5 / 8.9;   256, 500 14.7 / 10.5
-//   4 heads  d=64 8, 250 9.6 / 8.5;   8, 500 8.5 / 8.7;   d=128 8, 120 8.5 / 6.3;   8, 250 9.8 / 10.3;   8, 500 8.8 / 12.5;   256, 500 19.7 / 14.2
-//   8 heads  d=64 8, 120 10.6 / 10.5;   256, 250 13.5 / 15.2;   d=128 8, 120 12.3 / 10.3;   8, 250 12.6 / 18.6;   256, 250 15.6 / 20.2
+//   4 heads  d=64 8, 250 9.6 / 8.5;   8, 500 8.5 / 8.7;   d=128 8, 120 8.5 / 6.3;   8, 240 9.8 / 8.8;   8, 500 8.8 / 12.7;   256, 500 19.7 / 14.2
 static bool in_one(const SharedParams& p, int d) {
-  if (p.P > 0 || p.T > kOneRows) return false;
   const int G = p.Hq / p.Hk, step = kOneWaves * 4 * 512 / d;
+  if (p.P > 0 || p.T > kOneRows || G > 4) return false;
   const long long steps = ((long long)p.T + p.depth_count + step - 1) / step;
-  if (G > 4) return G <= 8 && d == 128 && steps <= 1;
-  if ((long long)p.B * p.Hk >= 128) return steps <= 4;
-  return steps <= (G == 1 ? 4 : G == 2 || d == 64 ? 2 : 1);
+  return steps <= (G == 1 || (long long)p.B * p.Hk >= 128 ? 4 : 2);
 }
 
 static size_t state_count(const SharedParams& p) { return ((size_t)p.B * p.Hq * p.n_slices + 1) / 2 * 2; }  // (even: 16-byte pieces)
@@ -796,24 +804,25 @@ size_t decode_shared_workspace_bytes(const SharedParams& dims, int d, bool with_
   SharedParams p = dims;
   plan(p, d);
   const Plan l(p, d);
-  long long own = p.T > 0 ? slices_wanted(p.T, l.own.units, l.own.many, l.own.good, l.own.least) : 0;
-  SharedParams alone = dims;  // (the same without a prefix)
-  alone.P = 0;
-  const Plan a(alone, d);
-  if (p.T > 0) own = std::max(own, slices_wanted(p.T, a.own.units, a.own.many, a.own.good, a.own.least));
+  long long own = 0;  // (whichever way they are read, with a prefix and without)
+  for (int heads : {0, l.own_heads > 0 ? l.own_heads : 4})
+    for (bool prefix : {false, true}) {
+      const Cut c = Plan::own_cut((long long)p.B * p.Hk, p.Hq / p.Hk, heads, prefix, kShWaves * 4 * 512 / d);
+      if (p.T > 0) own = std::max(own, slices_wanted(p.T, c.units, c.many, c.good, c.least));
+    }
   p.n_slices = (int)(std::max(own, 1ll) + (p.P > 0 ? slices_wanted(p.P, l.prefix.units, std::max(l.prefix.many, l.kind > 1 ? 512 : 0), l.prefix.good, l.prefix.least) : 0));
   return (state_count(p) * (d + 2) + (with_weights ? (size_t)p.B * p.Hq * p.score_step : 0)) * sizeof(float);
 }
 
 template <int D, int PREFIX>
 static void (*slices_kernel(int own))(SharedParams) {
-  return own == 2 ? moda_shared_slices_kernel<D, PREFIX, 2> : own == 1 ? moda_shared_slices_kernel<D, PREFIX, 1>
-                                                                       : moda_shared_slices_kernel<D, PREFIX, 0>;
+  return own == 4 ? moda_shared_slices_kernel<D, PREFIX, 4> : own == 2 ? moda_shared_slices_kernel<D, PREFIX, 2>
+         : own == 1 ? moda_shared_slices_kernel<D, PREFIX, 1> : moda_shared_slices_kernel<D, PREFIX, 0>;
 }
 
 template <int D>
 static hipError_t launch_d(const SharedParams& p, hipStream_t stream) {
-  const int G = p.Hq / p.Hk, own = own_kind(G);
+  const int G = p.Hq / p.Hk, own = own_kind(p);
   if (in_one(p, D)) {
     const long long groups = (long long)p.B * p.Hk;
     if (!grid_ok(groups, kOneWaves * 64)) return kGridTooLarge;

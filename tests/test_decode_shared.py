@@ -141,6 +141,15 @@ def test_ragged_lengths_and_weights(B, Hq, Hk, T, d, L, lens):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,Hq,Hk,T,d,P", [(8, 64, 8, 500, 64, 0), (7, 40, 8, 450, 128, 0), (16, 32, 8, 520, 128, 0), (16, 24, 8, 513, 64, 33),
+                                           (8, 64, 8, 400, 128, 65), (16, 24, 8, 520, 64, 0)])
+def test_many_own_rows_of_middling_groups(B, Hq, Hk, T, d, P):
+    """Groups of 3 to 8 heads take the matrix pipe with this many rows in all, the vector ALUs with fewer."""
+    lens = [T - 37 * i if i % 3 else i for i in range(B)]
+    check(B, Hq, Hk, T, d, 5, P, lens=lens, kv_alloc=T + 3, seed=B + T)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("B,Hq,Hk,T,d,L,lens", [
     (3, 10, 2, 100, 128, 4, [100, 0, 33]), (2, 8, 1, 121, 128, 7, [121, 1]), (2, 7, 1, 128, 128, 0, [128, 127]), (3, 8, 2, 300, 64, 5, [300, 299, 2]),
     (64, 4, 2, 512, 64, 1, None), (64, 2, 2, 511, 128, 0, None), (1, 1, 1, 1, 128, 0, [0]), (2, 4, 4, 0, 64, 9, None), (5, 6, 3, 255, 64, 1, [255, 256, 0, 64, 65]),
