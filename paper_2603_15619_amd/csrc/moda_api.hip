@@ -369,8 +369,12 @@ static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 
 static const moda_prefix kNoPrefix = {1, 0, 0};
 
+// Each call looks at the fields of the shape that it uses: the others are checked as fields that every call takes.
 static moda_status check_shared(const moda_prefix* x, const moda_shape* s) {
-  const moda_status st = check_dims(s);
+  if (!s) return MODA_ERR_NULL;
+  moda_shape used = *s;
+  used.causal = 0;
+  const moda_status st = check_dims(&used);
   if (st != MODA_OK) return st;
   if (s->dtype != MODA_BF16) return MODA_ERR_UNSUPPORTED;
   if (x->n_prefixes <= 0 || x->prefix_rows < 0 || x->prefix_alloc < x->prefix_rows) return MODA_ERR_SHAPE;
@@ -439,6 +443,13 @@ moda_status moda_attn_decode_weights(const void* Q, const void* Kseq, const void
                                  weights_out, O, LSE, kv_alloc, workspace, workspace_bytes, nullptr, s, hip_stream);
 }
 
+static moda_status check_weights(const moda_shape* s) {
+  if (!s) return MODA_ERR_NULL;
+  moda_shape used = *s;
+  used.depth_alloc = used.depth_count = 0;
+  return check_shape(&used);
+}
+
 static moda::WeightsParams weights_dims(int32_t window, const moda_shape* s) {
   moda::WeightsParams p{};
   p.B = s->B; p.Hq = s->Hq; p.Hk = s->Hk; p.T = s->T;
@@ -448,14 +459,14 @@ static moda::WeightsParams weights_dims(int32_t window, const moda_shape* s) {
 }
 
 size_t moda_attn_weights_workspace_bytes(int32_t window, const moda_shape* s) {
-  if (check_shape(s) != MODA_OK || window < 0 || s->B == 0 || s->T == 0) return 0;
+  if (check_weights(s) != MODA_OK || window < 0 || s->B == 0 || s->T == 0) return 0;
   return moda::weights_workspace_bytes(weights_dims(window, s), s->d, s->dtype == MODA_F32);
 }
 
 moda_status moda_attn_weights(const void* Q, const void* Kseq, const float* LSE, const int32_t* lengths,
                               const float* weights_in, float* weights_out, int32_t window, int32_t kv_alloc,
                               void* workspace, size_t workspace_bytes, const moda_shape* s, void* hip_stream) {
-  const moda_status st = check_shape(s);
+  const moda_status st = check_weights(s);
   if (st != MODA_OK) return st;
   if (window < 0 || kv_alloc < s->T) return MODA_ERR_SHAPE;
   if (s->B == 0 || s->T == 0) return MODA_OK;
@@ -474,8 +485,17 @@ moda_status moda_attn_weights(const void* Q, const void* Kseq, const float* LSE,
   return launch_status(moda::launch_weights(p, s->d, f32, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
+static moda_status check_evict(const moda_shape* s) {
+  if (!s) return MODA_ERR_NULL;
+  moda_shape used = *s;
+  used.Hq = s->Hk;
+  used.depth_alloc = used.depth_count = used.causal = 0;
+  used.scale = 0.f;
+  return check_dims(&used);
+}
+
 size_t moda_cache_evict_workspace_bytes(int32_t keep, const moda_shape* s) {
-  if (check_dims(s) != MODA_OK || keep < 1 || s->B == 0 || s->T < 1) return 0;
+  if (check_evict(s) != MODA_OK || keep < 1 || s->B == 0 || s->T < 1) return 0;
   return moda::evict_workspace_bytes(s->B, s->Hk, s->T, keep);
 }
 
@@ -484,7 +504,7 @@ moda_status moda_cache_evict(const void* Kseq, const void* Vseq, const float* we
                              int32_t* positions_out, int32_t* lengths_out, int32_t* index, int32_t keep,
                              int32_t recent, int32_t kv_alloc, int32_t out_alloc, void* workspace,
                              size_t workspace_bytes, const moda_shape* s, void* hip_stream) {
-  const moda_status st = check_dims(s);
+  const moda_status st = check_evict(s);
   if (st != MODA_OK) return st;
   if (s->T < 1 || keep < 1 || recent < 0 || recent > keep || kv_alloc < s->T) return MODA_ERR_SHAPE;
   const int n = std::min(keep, s->T);
