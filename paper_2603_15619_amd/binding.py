@@ -351,6 +351,14 @@ def _workspace(workspace, need, device):
     return workspace, workspace.numel() * workspace.element_size()
 
 
+def _int32(x, name):
+    """int(x), refused where the C ABI's 32 bits do not hold it (ctypes would drop the others)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError("%s: %d does not fit 32 bits" % (name, x))
+    return x
+
+
 def _decode_shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T, depth_count, scale,
                    weights, weights_out, out, lse, workspace):
     r = (_native_module or _native()).shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengths, lengths, P, T,
@@ -362,11 +370,11 @@ def _decode_shared(Q, Kprefix, Vprefix, Kseq, Vseq, Kdepth, Vdepth, prefix_lengt
         raise ValueError("Kseq or Kprefix must be given")
     Hk = (Kprefix if Kseq is None else Kseq).shape[1]
     kv_alloc = 0 if Kseq is None else Kseq.shape[2]
-    T = kv_alloc if T is None else int(T)
+    T = kv_alloc if T is None else _int32(T, "T")
     La = 0 if Kdepth is None else Kdepth.shape[2]
-    L = La if depth_count is None else int(depth_count)
+    L = La if depth_count is None else _int32(depth_count, "depth_count")
     Np, prefix_alloc = (1, 0) if Kprefix is None else (Kprefix.shape[0], Kprefix.shape[2])
-    P = prefix_alloc if P is None else int(P)
+    P = prefix_alloc if P is None else _int32(P, "P")
     dev, dt = Q.device, Q.dtype
     _require(Q, "Q", (B, Hq, d), dt, dev)
     _require(Kprefix, "Kprefix", (Np, Hk, prefix_alloc, d), dt, dev)
@@ -440,6 +448,7 @@ def moda_attn_weights(Q, Kseq, LSE, window=0, causal=True, scale=None, lengths=N
         return weights_out
     B, Hq, T, d = Q.shape
     Hk, kv_alloc = Kseq.shape[1], Kseq.shape[2]
+    window = _int32(window, "window")
     dev, dt = Q.device, Q.dtype
     _require(Q, "Q", (B, Hq, T, d), dt, dev)
     _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
@@ -448,11 +457,11 @@ def moda_attn_weights(Q, Kseq, LSE, window=0, causal=True, scale=None, lengths=N
     _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
     _require(weights_out, "weights_out", (B, Hk, kv_alloc), torch.float32, dev)
     s = MODAShape(B, Hq, Hk, T, d, 0, 0, int(bool(causal)), float(scale) if scale else 0.0, _dtype_code(Q))
-    need = int(lib().moda_attn_weights_workspace_bytes(int(window), ctypes.byref(s))) if workspace is None else 0
+    need = int(lib().moda_attn_weights_workspace_bytes(window, ctypes.byref(s))) if workspace is None else 0
     workspace, ws_bytes = _workspace(workspace, need, dev)
     with torch.cuda.device(dev):
         _check(lib().moda_attn_weights(_ptr(Q), _ptr(Kseq), _ptr(LSE), _ptr(lengths), _ptr(weights), _ptr(weights_out),
-                                       int(window), kv_alloc, _ptr(workspace), ws_bytes, ctypes.byref(s), _stream(dev)))
+                                       window, kv_alloc, _ptr(workspace), ws_bytes, ctypes.byref(s), _stream(dev)))
     return weights_out
 
 
@@ -465,8 +474,9 @@ def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, length
     positions_out or None) of out_alloc >= min(keep, T) rows, there.  index: the row that each came from, -1 behind them.
     Without lengths_out a call in place overwrites `lengths`, if given; else the new lengths are a new tensor."""
     B, Hk, kv_alloc, d = Kseq.shape
-    T = kv_alloc if T is None else int(T)
-    keep, n = int(keep), max(0, min(int(keep), T))
+    T = kv_alloc if T is None else _int32(T, "T")
+    keep = _int32(keep, "keep")
+    n = max(0, min(keep, T))
     dev, dt = Kseq.device, Kseq.dtype
     Kout, Vout, W_out, P_out = (Kseq, Vseq, weights, positions) if out is None else out
     if Kout.dim() != 4:
@@ -481,6 +491,7 @@ def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, length
     if r is not None:
         _outputs(r)
         return index, lengths_out
+    recent = _int32(recent, "recent")
     _require(Kseq, "Kseq", (B, Hk, kv_alloc, d), dt, dev)
     _require(Vseq, "Vseq", (B, Hk, kv_alloc, d), dt, dev)
     _require(weights, "weights", (B, Hk, kv_alloc), torch.float32, dev)
@@ -498,7 +509,7 @@ def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, length
     with torch.cuda.device(dev):
         _check(lib().moda_cache_evict(
             _ptr(Kseq), _ptr(Vseq), _ptr(weights), _ptr(positions), _ptr(lengths), _ptr(Kout), _ptr(Vout), _ptr(W_out),
-            _ptr(P_out), _ptr(lengths_out), _ptr(index), keep, int(recent), kv_alloc, out_alloc, _ptr(workspace), ws_bytes,
+            _ptr(P_out), _ptr(lengths_out), _ptr(index), keep, recent, kv_alloc, out_alloc, _ptr(workspace), ws_bytes,
             ctypes.byref(s), _stream(dev)))
     return index, lengths_out
 

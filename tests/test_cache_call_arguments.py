@@ -1,4 +1,5 @@
-"""Arguments of the calls on a shared or bounded cache that few callers pass: shape fields that a call does not use."""
+"""Arguments of the calls on a shared or bounded cache that few callers pass: shape fields that a call does not use, numbers that
+do not fit the C ABI's."""
 import ctypes
 
 import pytest
@@ -53,3 +54,25 @@ def test_workspace_sizes_look_at_the_fields_in_use_only():
             if field not in USED_BY[uses]:
                 for v in values:
                     assert size(ctypes.byref(MODAShape(**dict(b, **{field: v})))) == want, (uses, field, v)
+
+
+def test_numbers_that_do_not_fit_32_bits_are_refused():
+    """2^32 + 5 rows to keep are not 5.  (On the host: numbers are looked at before tensors.)"""
+    import torch
+
+    from paper_2603_15619_amd import moda_attn_decode_shared, moda_attn_decode_weights, moda_attn_weights, moda_cache_evict
+
+    t, w = torch.zeros(2, 2, 8, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 8)
+    q = t[:, :, 0].contiguous()
+    calls = {"keep": lambda n: moda_cache_evict(t, t, w, n), "recent": lambda n: moda_cache_evict(t, t, w, 6, recent=n),
+             "T": lambda n: moda_cache_evict(t, t, w, 6, T=n), "window": lambda n: moda_attn_weights(t, t, w, window=n, weights_out=w)}
+    for n in (1 << 31, (1 << 32) + 5, -(1 << 32) + 5, -(1 << 31) - 1, 1 << 70):
+        for name, call in calls.items():
+            with pytest.raises(ValueError, match="%s: .*32 bits" % name):
+                call(n)
+        for name in ("P", "T", "depth_count"):
+            with pytest.raises(ValueError, match="%s: .*32 bits" % name):
+                moda_attn_decode_shared(q, t, t, t, t, t, t, **{name: n})
+        for name in ("T", "depth_count"):
+            with pytest.raises(ValueError, match="%s: .*32 bits" % name):
+                moda_attn_decode_weights(q, t, t, w, t, t, **{name: n})
