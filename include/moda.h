@@ -245,6 +245,10 @@ typedef struct {
  *        grows: what it is for the longest caches serves shorter ones.
  * A token that sees nothing (all lengths 0, no slots), or whose logits are all -inf, gets O = 0, LSE = -inf and
  * adds no weight.  s->causal is ignored.  bf16 only.  kv_alloc >= s->T >= 0.
+ * Logits, references, normalisers, sums and accumulated weights are fp32.  The softmax weights that multiply the values are rounded to
+ * bf16 where the matrix pipe takes them: prefixes that more than 4 queries of a key/value head share, own rows of groups of more than 8
+ * heads, and of 3 to 8 where the caches together are long.  Elsewhere they are fp32.
+ * The workspace is required of every call, also of one short enough to leave it untouched.
  */
 size_t moda_attn_decode_shared_workspace_bytes(const moda_prefix* prefix, int with_weights, const moda_shape* s);
 moda_status moda_attn_decode_shared(const void* Q, const void* Kprefix, const void* Vprefix, const void* Kseq,
@@ -269,6 +273,9 @@ moda_status moda_attn_decode_weights(const void* Q, const void* Kseq, const void
  *                        (t >= j where causal) of exp(scale * <Q[b,h,t], Kseq[b,g,j]> - LSE[b,h,t])
  * for j < length of b, over the queries t < length of b; window > 0: over the last `window` of them only (0: all).
  * With depth slots the LSE of the forward pass covers them too, and the weights are those of that softmax.
+ * The LSE is taken as it is: a query's weights sum to one over the keys that its LSE covers.  With causal == 1 those of the queries
+ * t < length cover filled rows only.  With causal == 0 and `lengths` the LSE has to leave the rows behind a length out, which that of
+ * moda_attn_fwd on a padded batch does not.
  *   in : Q [B, Hq, T, d]; Kseq [B, Hk, kv_alloc, d], kv_alloc >= T; LSE [B, Hq, T] fp32; lengths [B] or NULL;
  *        weights_in [B, Hk, kv_alloc] fp32 or NULL
  *   out: weights_out [B, Hk, kv_alloc] fp32

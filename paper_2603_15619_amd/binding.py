@@ -439,7 +439,7 @@ def moda_attn_weights(Q, Kseq, LSE, window=0, causal=True, scale=None, lengths=N
     """weights [B,Hk,kv_alloc] (fp32): the attention weight that each row of Kseq [B,Hk,kv_alloc,d] gets from the queries
     Q [B,Hq,T,d] (T <= kv_alloc) whose log-sum-exp LSE [B,Hq,T] the forward pass left, summed over queries and the heads of
     a group; of the last `window` queries only unless that is 0.  lengths [B] (int32): the filled positions of each
-    sequence.  Added to `weights` where given, in place unless weights_out is."""
+    sequence (causal=False: LSE has to leave the others out, which moda_attn_fwd on a padded batch does not).  Added to `weights` where given, in place unless weights_out is."""
     if weights_out is None:
         weights_out = weights if weights is not None else torch.zeros(Kseq.shape[:3], dtype=torch.float32, device=Q.device)
     r = (_native_module or _native()).weights(Q, Kseq, LSE, window, causal, scale, lengths, weights, weights_out, workspace)

@@ -319,7 +319,9 @@ struct Columns {
           pv[i] = fast_exp2(s[b][hf * 8 + i] * c2 - mc);
           l += pv[i];
         }
-        // weights as bf16 for the matrix pipe: off by 2^-8 of themselves at most, the normaliser is summed before
+        // weights as bf16, the type of the matrix pipe's operands: off by 2^-8 of themselves at most, and not all one way; the normaliser is
+        // summed before.  (Outputs of N(0,1) data are off by 0.0023 of their size for it, 0.0017 with fp32 weights, which is O's own
+        // rounding.  A second product for what the rounding leaves would double the matrix work on values.)
         const bf16x8 pb = pack8(pv);
 #pragma unroll
         for (int cb = 0; cb < Tl::kDBlocks; ++cb)
@@ -716,6 +718,7 @@ __global__ __launch_bounds__(256) void moda_shared_finish_kernel(SharedParams p,
 //   d=64   8, 600 8.4 / 10.1;   8, 5000 10.5 / 12.5;   32, 1200 10.1 / 12.0;   32, 2500 12.9 / 13.1;   8, 12000 14.0 / 13.8;   128, 5000 37.8 / 36.0
 //   d=128  8, 600 8.6 / 11.9;   8, 5000 12.6 / 14.7;   32, 1200 11.9 / 14.5;   32, 2500 18.1 / 15.9;   8, 12000 20.3 / 16.8;   512, 2500 127 / 120
 //   8 heads, in two workgroups:  d=64 8, 1200 8.9 / 10.4;   8, 2500 10.4 / 11.0;   8, 5000 13.3 / 12.6;   d=128 8, 1200 10.9 / 12.4;   8, 5000 19.0 / 14.8
+// (One limit for both head dimensions: d = 64 would go on a little longer, 32 x 2500 rows are 0.2 us behind.)
 static int own_kind(const SharedParams& p) {
   const int G = p.Hq / p.Hk;
   if (G <= 2) return G;
@@ -790,6 +793,8 @@ static void plan(SharedParams& p, int d) {
 //   1 head   d=64 16, 20 7.1 / 4.7;   64, 500 7.2 / 5.4;   512, 500 13.8 / 9.8;   d=128 16, 250 7.8 / 6.7;   16, 500 7.2 / 7.6;   512, 500 23.0 / 18.5
 //   2 heads  d=64 8, 500 7.5 / 6.5;   d=128 8, 120 7.3 / 4.9;   8, 250 8.1 / 7.5;   8, 500 7.5 / 8.9;   256, 500 14.7 / 10.5
 //   4 heads  d=64 8, 250 9.6 / 8.5;   8, 500 8.5 / 8.7;   d=128 8, 120 8.5 / 6.3;   8, 240 9.8 / 8.8;   8, 500 8.8 / 12.7;   256, 500 19.7 / 14.2
+// (The limits in steps are the same for both head dimensions; where they end the one kernel may be a little behind: 1 head d=128 16 x 500, 4
+// heads d=64 8 x 500.)
 static bool in_one(const SharedParams& p, int d) {
   const int G = p.Hq / p.Hk, step = kOneWaves * 4 * 512 / d;
   if (p.P > 0 || p.T > kOneRows || G > 4) return false;
