@@ -312,6 +312,98 @@ moda_status moda_cache_evict(const void* Kseq, const void* Vseq, const float* we
                              size_t workspace_bytes, const moda_shape* s, void* hip_stream);
 
 /*
+ * A paged sequence cache.  The rows of all sequences lie in pages of one pool for keys and one for values; a table gives every sequence its
+ * pages in the order of its rows, so that sequences take and give back memory page by page.
+ *
+ *   Kpages, Vpages    [n_pages, Hk, page_rows, d]       bf16, or 8-bit floats (e4m3: finite, largest 448)
+ *   Kscales, Vscales  [n_pages, Hk, page_rows, d / 32]  8-bit pages only (NULL else): per 32 channels of a row an exponent + 127
+ *   Kbounds           [n_pages, Hk, 2, d]               bf16: the least and the largest value of every key channel of a page
+ *   page_table        [B, max_pages] int32, device: row r of sequence b lies in row r % page_rows of page
+ *                     page_table[b, r / page_rows].  An entry outside [0, n_pages) is no page: its rows take no part in anything (a sequence
+ *                     that has given back its oldest rows).  A page may stand in several sequences' tables (a prefix that they
+ *                     share) as long as none of them writes it.
+ *   lengths           [B] int32, device, 4-byte aligned, or NULL: the rows of each sequence, counted from row 0, missing pages included
+ *
+ * 8-bit pages: a scale is 2^e with the least e >= -100 for which the largest of the 32 finite magnitudes is at most 448 * 2^e; a channel
+ * is held as e4m3(x / 2^e), rounded to nearest even, and stands for that times 2^e: off by 2^-4 of itself, or by 2^(e - 10) where it
+ * is below 2^(e - 6).  bf16 holds every such value exactly.  Numbers that are not finite are held as NaN; magnitudes above
+ * 1.875 * 2^127 as that.
+ *
+ * Of the shape every call uses B, Hk, d (64 or 128), dtype (MODA_BF16: type of everything but the pages) and what it names below;
+ * page_rows: 16, 32, 64, 128 or 256; max_pages * page_rows <= 2^30 (MODA_ERR_UNSUPPORTED above).  No call synchronises or reads
+ * the table on the host.
+ */
+typedef enum { MODA_PAGES_BF16 = 0, MODA_PAGES_MX8 = 1 } moda_pages_type;
+typedef struct {
+  int32_t n_pages;   /* pages of the pools, > 0           */
+  int32_t page_rows; /* rows of a page                    */
+  int32_t max_pages; /* columns of the page table, > 0    */
+  int32_t type;      /* a moda_pages_type                 */
+} moda_pages;
+
+/*
+ * New rows go to their places in the pages, quantised where the pages hold 8 bits.  After the call sequence b has lengths[b] rows (NULL:
+ * T), of which the last n_b = min(T, counts[b], lengths[b]) (counts NULL: min(T, lengths[b])) are written: row r of K, V becomes row
+ * lengths[b] - n_b + r.  Rows whose place the table does not have are left out.  A decoding step has T = 1 and the lengths that its attention
+ * takes; a padded batch of prompts their lengths, and counts NULL.
+ *   in : K, V [B, Hk, T, d]; page_table; lengths, counts [B] or NULL
+ *   out: Kpages, Vpages, Kscales, Vscales: the rows written, nothing else; Kbounds or NULL: of the pages written, the bounds of the rows of
+ *        this call (as stored), together with what Kbounds holds unless row 0 of the page is among them.  A NaN among the keys makes both
+ *        bounds of its channel NaN.
+ * A page that the call writes stands once in all tables.  Uses T of the shape.
+ */
+moda_status moda_page_append(const void* K, const void* V, const int32_t* page_table, const int32_t* lengths, const int32_t* counts,
+                             void* Kpages, void* Vpages, void* Kscales, void* Vscales, void* Kbounds, const moda_pages* x,
+                             const moda_shape* s, void* hip_stream);
+
+/*
+ * Rows [first, first + T) of every sequence as one array again: what the pages hold, exactly.
+ *   in : Kpages, Vpages, Kscales, Vscales, page_table, lengths [B] or NULL (all rows that the table has)
+ *   out: K, V [B, Hk, T, d]: row r is row first + r of its sequence; rows from a sequence's length on, or of pages that it does not
+ *        have, are left as they were
+ * first >= 0, first + T <= 2^30.  Uses T of the shape.
+ */
+moda_status moda_page_read(const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales, const int32_t* page_table,
+                           const int32_t* lengths, void* K, void* V, int32_t first, const moda_pages* x, const moda_shape* s,
+                           void* hip_stream);
+
+/*
+ * The pages that a decoding step reads when it does not read all: for each (sequence, key/value head) the `first` first and `recent` last of the
+ * ceil(length / page_rows) pages of the sequence and, up to `keep` in all, those with the largest
+ *   score = sum over the channels c of up_c * max_c + down_c * min_c,
+ *   up_c = sum over the heads of the group of max(Q_c, 0), down_c = that of min(Q_c, 0), min and max the page's bounds:
+ * no row of the page has a larger sum of <Q_h, k> over the group's heads.  Ties go to the lowest page; a NaN score counts as above all
+ * others.  Scores are formed in 64 bits.  Pages that the table does not have are never chosen.
+ *   in : Q [B, Hq, d]; Kbounds; page_table; lengths [B] or NULL (all T), read as for the decoding step
+ *   out: pages [B, Hk, keep] int32: indices into the sequence's table, ascending, -1 behind the last
+ *   workspace: at least moda_page_select_workspace_bytes(x, s) bytes (may be 0: then NULL is accepted), 16-byte aligned
+ * keep >= 1, first, recent >= 0, first + recent <= keep.  Uses Hq and T of the shape: T bounds the lengths, max_pages * page_rows >= T >= 0.
+ */
+size_t moda_page_select_workspace_bytes(const moda_pages* x, const moda_shape* s);
+moda_status moda_page_select(const void* Q, const void* Kbounds, const int32_t* page_table, const int32_t* lengths, int32_t* pages,
+                             int32_t keep, int32_t first, int32_t recent, void* workspace, size_t workspace_bytes, const moda_pages* x,
+                             const moda_shape* s, void* hip_stream);
+
+/*
+ * Decoding step over a paged cache: for each of the B new tokens ONE softmax over the rows of its sequence's pages and its depth slots;
+ * the new token's own key and value are among the rows already (moda_page_append).
+ *   in : Q [B, Hq, d]; Kpages, Vpages, Kscales, Vscales; page_table; lengths [B] or NULL (all T)
+ *        selected          [B, Hk, n_selected] int32 or NULL: only the rows of these pages (indices into the sequence's table, each once; others
+ *                          than its pages, e.g. -1, name nothing)
+ *        Kdepth, Vdepth    [B, Hk, depth_alloc, d] (NULL allowed iff depth_count == 0), always bf16
+ *   out: O [B, Hq, d], LSE [B, Hq] fp32, over the rows that are read
+ *   workspace: at least moda_attn_decode_paged_workspace_bytes(x, s) bytes, 16-byte aligned; does not depend on T
+ * A token that sees nothing, or whose logits are all -inf, gets O = 0, LSE = -inf.  Uses Hq, T (bounds the lengths: one below 0 counts as 0, one
+ * above T as T; max_pages * page_rows >= T >= 0), depth_alloc, depth_count and scale of the shape.  Logits, references, normalisers and
+ * sums are fp32.
+ */
+size_t moda_attn_decode_paged_workspace_bytes(const moda_pages* x, const moda_shape* s);
+moda_status moda_attn_decode_paged(const void* Q, const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales,
+                                   const int32_t* page_table, const int32_t* lengths, const int32_t* selected, int32_t n_selected,
+                                   const void* Kdepth, const void* Vdepth, void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                                   const moda_pages* x, const moda_shape* s, void* hip_stream);
+
+/*
  * Measurement aid: a kernel whose loop holds nothing but the bf16 matrix instruction the
  * attention kernels use (v_mfma_f32_32x32x16_bf16; eight waves per workgroup, four independent
  * accumulators per wave), for reporting what the matrix pipe of THIS chip sustains next to its

@@ -21,12 +21,15 @@ LIB_PATH = os.environ.get("MODA_LIB_PATH") or os.path.join(HERE, "libmoda.so")
 NATIVE_PATH = os.path.join(HERE, "moda_torch.so")
 
 MODA_F32, MODA_BF16 = 0, 1
+MODA_PAGES_BF16, MODA_PAGES_MX8 = 0, 1
 EXPORTS = ("moda_attn_fwd", "moda_attn_fwd_tuned", "moda_attn_bwd_workspace_bytes", "moda_attn_bwd", "moda_depth_append",
            "moda_attn_decode", "moda_attn_decode_workspace_bytes", "moda_attn_decode_noalloc",
            "moda_attn_decode_noalloc_max_bytes",
            "moda_attn_decode_shared", "moda_attn_decode_shared_workspace_bytes", "moda_attn_decode_weights",
            "moda_attn_weights", "moda_attn_weights_workspace_bytes",
            "moda_cache_evict", "moda_cache_evict_workspace_bytes",
+           "moda_page_append", "moda_page_read", "moda_page_select", "moda_page_select_workspace_bytes",
+           "moda_attn_decode_paged", "moda_attn_decode_paged_workspace_bytes",
            "moda_calibrate_mfma", "moda_calibrate_mfma_operand_bytes", "moda_calibrate_mfma_sink_bytes",
            "moda_status_string", "moda_version", "moda_kernels_per_call", "moda_fwd_kernel_name",
            "moda_bwd_kernel_name")
@@ -46,6 +49,10 @@ class MODAFwdTuning(ctypes.Structure):
 
 class MODAPrefix(ctypes.Structure):
     _fields_ = [("n_prefixes", ctypes.c_int32), ("prefix_rows", ctypes.c_int32), ("prefix_alloc", ctypes.c_int32)]
+
+
+class MODAPages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("type", ctypes.c_int32)]
 
 
 class MODAError(RuntimeError):
@@ -100,6 +107,19 @@ def lib():
         L.moda_cache_evict_workspace_bytes.restype = size
         L.moda_cache_evict.argtypes = [vp] * 11 + [i32] * 4 + [vp, size, sp, vp]
         L.moda_cache_evict.restype = ctypes.c_int
+        gp = ctypes.POINTER(MODAPages)
+        L.moda_page_append.argtypes = [vp] * 10 + [gp, sp, vp]
+        L.moda_page_append.restype = ctypes.c_int
+        L.moda_page_read.argtypes = [vp] * 8 + [i32, gp, sp, vp]
+        L.moda_page_read.restype = ctypes.c_int
+        L.moda_page_select_workspace_bytes.argtypes = [gp, sp]
+        L.moda_page_select_workspace_bytes.restype = size
+        L.moda_page_select.argtypes = [vp] * 5 + [i32, i32, i32, vp, size, gp, sp, vp]
+        L.moda_page_select.restype = ctypes.c_int
+        L.moda_attn_decode_paged_workspace_bytes.argtypes = [gp, sp]
+        L.moda_attn_decode_paged_workspace_bytes.restype = size
+        L.moda_attn_decode_paged.argtypes = [vp] * 8 + [i32] + [vp] * 5 + [size, gp, sp, vp]
+        L.moda_attn_decode_paged.restype = ctypes.c_int
         L.moda_calibrate_mfma_operand_bytes.argtypes = []
         L.moda_calibrate_mfma_operand_bytes.restype = ctypes.c_size_t
         L.moda_calibrate_mfma_sink_bytes.argtypes = [ctypes.c_int32]
@@ -512,6 +532,150 @@ def moda_cache_evict(Kseq, Vseq, weights, keep, recent=0, positions=None, length
             _ptr(P_out), _ptr(lengths_out), _ptr(index), keep, recent, kv_alloc, out_alloc, _ptr(workspace), ws_bytes,
             ctypes.byref(s), _stream(dev)))
     return index, lengths_out
+
+
+def _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, device):
+    """The pools' shape, MODAPages and (n_pages, Hk, page_rows, d): bf16 pools without scales, or e4m3 pools with both."""
+    if Kpages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("expected Kpages [n_pages,Hk,page_rows,d] and page_table [B,max_pages]")
+    n, Hk, R, d = Kpages.shape
+    mx = Kpages.dtype == torch.float8_e4m3fn
+    if not mx and Kpages.dtype != torch.bfloat16:
+        raise TypeError("pages hold bf16 or float8_e4m3fn, got %s" % Kpages.dtype)
+    if mx != (Kscales is not None) or mx != (Vscales is not None):
+        raise ValueError("Kscales and Vscales belong to float8_e4m3fn pages, and to them only")
+    max_pages = page_table.shape[1]
+    _require(Kpages, "Kpages", (n, Hk, R, d), Kpages.dtype, device)
+    _require(Vpages, "Vpages", (n, Hk, R, d), Kpages.dtype, device)
+    _require(Kscales, "Kscales", (n, Hk, R, d // 32), torch.uint8, device)
+    _require(Vscales, "Vscales", (n, Hk, R, d // 32), torch.uint8, device)
+    _require(page_table, "page_table", (B, max_pages), torch.int32, device)
+    return MODAPages(_int32(n, "n_pages"), _int32(R, "page_rows"), _int32(max_pages, "max_pages"), MODA_PAGES_MX8 if mx else MODA_PAGES_BF16)
+
+
+def _bound(T, page_table, page_rows):
+    """Rows that lengths may reach: T, or (None) all that the table has."""
+    return _int32(page_table.shape[1] * page_rows if T is None else T, "T")
+
+
+def moda_page_append(K, V, Kpages, Vpages, page_table, lengths=None, counts=None, Kscales=None, Vscales=None, Kbounds=None):
+    """New rows K, V [B,Hk,T,d] go to their places in the pages of a paged cache, in place: Kpages/Vpages [n_pages,Hk,page_rows,d] in
+    bf16, or in float8_e4m3fn with Kscales/Vscales [n_pages,Hk,page_rows,d/32] (uint8 exponents + 127); page_table [B,max_pages]
+    (int32): the page of each page_rows rows of a sequence, -1: none.  lengths [B] (int32; None: T): the rows of each sequence after
+    the call, of which the last min(T, counts [B], length) are the new ones.  Kbounds [n_pages,Hk,2,d] (bf16): the least and
+    largest key channels of every page written are kept there.  Returns Kpages, Vpages."""
+    B, Hk, T, d = K.shape
+    dev = K.device
+    x = _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, dev)
+    if Kpages.shape[1] != Hk or Kpages.shape[3] != d:
+        raise ValueError("Kpages: expected %d heads of dimension %d, got %s" % (Hk, d, tuple(Kpages.shape)))
+    _require(K, "K", (B, Hk, T, d), torch.bfloat16, dev)
+    _require(V, "V", (B, Hk, T, d), torch.bfloat16, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    _require(counts, "counts", (B,), torch.int32, dev)
+    _require(Kbounds, "Kbounds", (x.n_pages, Hk, 2, d), torch.bfloat16, dev)
+    s = MODAShape(B, Hk, Hk, _int32(T, "T"), d, 0, 0, 1, 0.0, MODA_BF16)
+    with torch.cuda.device(dev):
+        _check(lib().moda_page_append(_ptr(K), _ptr(V), _ptr(page_table), _ptr(lengths), _ptr(counts), _ptr(Kpages), _ptr(Vpages),
+                                      _ptr(Kscales), _ptr(Vscales), _ptr(Kbounds), ctypes.byref(x), ctypes.byref(s), _stream(dev)))
+    return Kpages, Vpages
+
+
+def moda_page_read(Kpages, Vpages, page_table, lengths=None, first=0, T=None, Kscales=None, Vscales=None, out=None):
+    """K, V [B,Hk,T,d] (bf16): rows [first, first + T) of every sequence of a paged cache (moda_page_append has its arguments), exactly as the
+    pages hold them.  T None: that of `out`, else all rows that the table has from `first` on.  Rows from a sequence's
+    length on (lengths [B]; None: all are there) and those of missing pages are left as they were in out = (K, V); without
+    `out` they are zero."""
+    B, dev = page_table.shape[0], Kpages.device
+    x = _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, dev)
+    Hk, d = Kpages.shape[1], Kpages.shape[3]
+    first = _int32(first, "first")
+    if T is None:
+        T = out[0].shape[2] if out is not None else max(0, x.max_pages * x.page_rows - first)
+    T = _int32(T, "T")
+    if T < 0:
+        raise ValueError("T: %d rows" % T)
+    if out is None:
+        out = tuple(torch.zeros((B, Hk, T, d), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    K, V = out
+    _require(K, "K", (B, Hk, T, d), torch.bfloat16, dev)
+    _require(V, "V", (B, Hk, T, d), torch.bfloat16, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    s = MODAShape(B, Hk, Hk, T, d, 0, 0, 1, 0.0, MODA_BF16)
+    with torch.cuda.device(dev):
+        _check(lib().moda_page_read(_ptr(Kpages), _ptr(Vpages), _ptr(Kscales), _ptr(Vscales), _ptr(page_table), _ptr(lengths), _ptr(K),
+                                    _ptr(V), first, ctypes.byref(x), ctypes.byref(s), _stream(dev)))
+    return K, V
+
+
+def moda_page_select(Q, Kbounds, page_table, keep, page_rows, lengths=None, first=1, recent=1, T=None, out=None, workspace=None):
+    """pages [B,Hk,keep] (int32): for each (sequence, key/value head) the `first` first and `recent` last pages and those whose key bounds
+    Kbounds [n_pages,Hk,2,d] promise the largest logits, summed over the heads of the group, for the queries Q [B,Hq,d]; indices into
+    the sequence's row of page_table [B,max_pages], ascending, -1 behind the last.  lengths [B] (int32; None: T, None: all rows that the
+    table has).  What moda_attn_decode_paged takes as `selected`."""
+    B, Hq, d = Q.shape
+    dev = Q.device
+    if Kbounds.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("expected Kbounds [n_pages,Hk,2,d] and page_table [B,max_pages]")
+    n, Hk, max_pages = Kbounds.shape[0], Kbounds.shape[1], page_table.shape[1]
+    keep, first, recent, page_rows = _int32(keep, "keep"), _int32(first, "first"), _int32(recent, "recent"), _int32(page_rows, "page_rows")
+    T = _bound(T, page_table, page_rows)
+    _require(Q, "Q", (B, Hq, d), torch.bfloat16, dev)
+    _require(Kbounds, "Kbounds", (n, Hk, 2, d), torch.bfloat16, dev)
+    _require(page_table, "page_table", (B, max_pages), torch.int32, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    if out is None:
+        out = torch.empty((B, Hk, max(keep, 0)), dtype=torch.int32, device=dev)
+    _require(out, "out", (B, Hk, keep), torch.int32, dev)
+    x = MODAPages(_int32(n, "n_pages"), page_rows, _int32(max_pages, "max_pages"), MODA_PAGES_BF16)
+    s = MODAShape(B, Hq, Hk, T, d, 0, 0, 1, 0.0, MODA_BF16)
+    need = int(lib().moda_page_select_workspace_bytes(ctypes.byref(x), ctypes.byref(s))) if workspace is None else 0
+    workspace, ws_bytes = _workspace(workspace, need, dev)
+    with torch.cuda.device(dev):
+        _check(lib().moda_page_select(_ptr(Q), _ptr(Kbounds), _ptr(page_table), _ptr(lengths), _ptr(out), keep, first, recent,
+                                      _ptr(workspace), ws_bytes, ctypes.byref(x), ctypes.byref(s), _stream(dev)))
+    return out
+
+
+def moda_attn_decode_paged(Q, Kpages, Vpages, page_table, Kdepth=None, Vdepth=None, lengths=None, selected=None, Kscales=None,
+                           Vscales=None, T=None, depth_count=None, scale=None, out=None, lse=None, workspace=None):
+    """O [B,Hq,d], LSE [B,Hq] for one new token per sequence, under one softmax over the rows of its pages (moda_page_append has
+    the cache's arguments; the token's own row is among them) and its depth slots Kdepth/Vdepth [B,Hk,depth_alloc,d] or None.
+    lengths [B] (int32): the rows of each sequence; T bounds them (default: all rows that the table has) and is their number where lengths is
+    None.  selected [B,Hk,n] (int32): only the rows of these pages, indices into the sequence's row of page_table, each once, -1: none."""
+    B, Hq, d = Q.shape
+    dev = Q.device
+    x = _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, dev)
+    Hk = Kpages.shape[1]
+    if Kpages.shape[3] != d:
+        raise ValueError("Kpages: expected a head dimension of %d, got %s" % (d, tuple(Kpages.shape)))
+    T = _bound(T, page_table, x.page_rows)
+    La = 0 if Kdepth is None else Kdepth.shape[2]
+    L = La if depth_count is None else _int32(depth_count, "depth_count")
+    _require(Q, "Q", (B, Hq, d), torch.bfloat16, dev)
+    _require(Kdepth, "Kdepth", (B, Hk, La, d), torch.bfloat16, dev)
+    _require(Vdepth, "Vdepth", (B, Hk, La, d), torch.bfloat16, dev)
+    _require(lengths, "lengths", (B,), torch.int32, dev)
+    n_selected = 0
+    if selected is not None:
+        if selected.dim() != 3 or selected.shape[2] == 0:
+            raise ValueError("selected: expected a [B,Hk,n] tensor, n > 0")
+        n_selected = _int32(selected.shape[2], "n_selected")
+        _require(selected, "selected", (B, Hk, n_selected), torch.int32, dev)
+    if out is None:
+        out = torch.empty_like(Q)
+    if lse is None:
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=dev)
+    _require(out, "out", Q.shape, torch.bfloat16, dev)
+    _require(lse, "lse", (B, Hq), torch.float32, dev)
+    s = MODAShape(B, Hq, Hk, T, d, La, L, 1, float(scale) if scale else 0.0, MODA_BF16)
+    need = int(lib().moda_attn_decode_paged_workspace_bytes(ctypes.byref(x), ctypes.byref(s))) if workspace is None else 0
+    workspace, ws_bytes = _workspace(workspace, need, dev)
+    with torch.cuda.device(dev):
+        _check(lib().moda_attn_decode_paged(
+            _ptr(Q), _ptr(Kpages), _ptr(Vpages), _ptr(Kscales), _ptr(Vscales), _ptr(page_table), _ptr(lengths), _ptr(selected), n_selected,
+            _ptr(Kdepth), _ptr(Vdepth), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes, ctypes.byref(x), ctypes.byref(s), _stream(dev)))
+    return out, lse
 
 
 def moda_calibrate_mfma(operands, workgroups, iters, sink=None):

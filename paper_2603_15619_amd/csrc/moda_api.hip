@@ -532,6 +532,176 @@ moda_status moda_cache_evict(const void* Kseq, const void* Vseq, const float* we
   return launch_status(moda::launch_evict(p, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
+// ---------------------------------------------------------------- a paged sequence cache
+// Which fields of the shape a call looks at beside B, Hk, d and dtype.
+enum { kUsesHeads = 1, kUsesT = 2, kUsesDepth = 4 };
+
+static moda_status check_pages(const moda_pages* x, const moda_shape* s, int uses) {
+  if (!x || !s) return MODA_ERR_NULL;
+  moda_shape used = *s;
+  used.causal = 0;
+  if (!(uses & kUsesHeads)) used.Hq = s->Hk;
+  if (!(uses & kUsesT)) used.T = 0;
+  if (!(uses & kUsesDepth)) {
+    used.depth_alloc = used.depth_count = 0;
+    used.scale = 0.f;
+  }
+  const moda_status st = check_dims(&used);
+  if (st != MODA_OK) return st;
+  if (s->dtype != MODA_BF16) return MODA_ERR_UNSUPPORTED;
+  if (x->n_pages <= 0 || x->max_pages <= 0 || x->page_rows <= 0) return MODA_ERR_SHAPE;
+  if (x->type != MODA_PAGES_BF16 && x->type != MODA_PAGES_MX8) return MODA_ERR_UNSUPPORTED;
+  if (x->page_rows < 16 || x->page_rows > 256 || (x->page_rows & (x->page_rows - 1))) return MODA_ERR_UNSUPPORTED;
+  if ((long long)x->max_pages * x->page_rows > 1ll << 30) return MODA_ERR_UNSUPPORTED;
+  return MODA_OK;
+}
+
+static int shift_of(const moda_pages* x) {
+  int shift = 4;
+  while (1 << shift < x->page_rows) ++shift;
+  return shift;
+}
+
+// The lengths of a decoding step or a choice of pages: T bounds them and fits the table.
+static moda_status check_length(const moda_pages* x, const moda_shape* s) {
+  return (long long)x->max_pages * x->page_rows < s->T ? MODA_ERR_SHAPE : MODA_OK;
+}
+
+// Pools and, with 8-bit pages, their scales.
+static moda_status check_pools(const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales, const moda_pages* x) {
+  if (!Kpages || !Vpages) return MODA_ERR_NULL;
+  if (x->type == MODA_PAGES_MX8 && (!Kscales || !Vscales)) return MODA_ERR_NULL;
+  for (const void* q : {Kpages, Vpages, Kscales, Vscales})
+    if (!aligned16(q)) return MODA_ERR_ALIGN;
+  return MODA_OK;
+}
+
+static moda::PageRowsParams page_rows_dims(const moda_pages* x, const moda_shape* s) {
+  moda::PageRowsParams p{};
+  p.B = s->B; p.Hk = s->Hk; p.T = s->T;
+  p.n_pages = x->n_pages; p.max_pages = x->max_pages; p.shift = shift_of(x);
+  return p;
+}
+
+moda_status moda_page_append(const void* K, const void* V, const int32_t* page_table, const int32_t* lengths, const int32_t* counts,
+                             void* Kpages, void* Vpages, void* Kscales, void* Vscales, void* Kbounds, const moda_pages* x,
+                             const moda_shape* s, void* hip_stream) {
+  moda_status st = check_pages(x, s, kUsesT);
+  if (st != MODA_OK) return st;
+  if (s->B == 0 || s->T == 0) return MODA_OK;
+  if (!K || !V || !page_table) return MODA_ERR_NULL;
+  if ((st = check_pools(Kpages, Vpages, Kscales, Vscales, x)) != MODA_OK) return st;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(Kbounds)) return MODA_ERR_ALIGN;
+  if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(counts)) return MODA_ERR_ALIGN;
+  moda::PageRowsParams p = page_rows_dims(x, s);
+  p.K = (const char*)K; p.V = (const char*)V;
+  p.table = page_table; p.lengths = lengths; p.counts = counts;
+  p.Kp = (char*)Kpages; p.Vp = (char*)Vpages; p.Ks = (unsigned char*)Kscales; p.Vs = (unsigned char*)Vscales;
+  p.bounds = (char*)Kbounds;
+  return launch_status(moda::launch_page_append(p, s->d, x->type == MODA_PAGES_MX8, static_cast<hipStream_t>(hip_stream)));
+}
+
+moda_status moda_page_read(const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales, const int32_t* page_table,
+                           const int32_t* lengths, void* K, void* V, int32_t first, const moda_pages* x, const moda_shape* s,
+                           void* hip_stream) {
+  moda_status st = check_pages(x, s, kUsesT);
+  if (st != MODA_OK) return st;
+  if (first < 0) return MODA_ERR_SHAPE;
+  if ((long long)first + s->T > 1ll << 30) return MODA_ERR_UNSUPPORTED;
+  if (s->B == 0 || s->T == 0) return MODA_OK;
+  if (!K || !V || !page_table) return MODA_ERR_NULL;
+  if ((st = check_pools(Kpages, Vpages, Kscales, Vscales, x)) != MODA_OK) return st;
+  if (!aligned16(K) || !aligned16(V) || !aligned4(page_table) || !aligned4(lengths)) return MODA_ERR_ALIGN;
+  moda::PageRowsParams p = page_rows_dims(x, s);
+  p.first = first;
+  p.table = page_table; p.lengths = lengths;
+  p.Kp = (char*)Kpages; p.Vp = (char*)Vpages; p.Ks = (unsigned char*)Kscales; p.Vs = (unsigned char*)Vscales;
+  p.K_out = (char*)K; p.V_out = (char*)V;
+  return launch_status(moda::launch_page_read(p, s->d, x->type == MODA_PAGES_MX8, static_cast<hipStream_t>(hip_stream)));
+}
+
+static moda_status check_select(const moda_pages* x, const moda_shape* s) {
+  const moda_status st = check_pages(x, s, kUsesHeads | kUsesT);
+  return st != MODA_OK ? st : check_length(x, s);
+}
+
+static moda::SelectParams select_dims(const moda_pages* x, const moda_shape* s) {
+  moda::SelectParams p{};
+  p.B = s->B; p.Hq = s->Hq; p.Hk = s->Hk; p.T = s->T;
+  p.n_pages = x->n_pages; p.max_pages = x->max_pages; p.shift = shift_of(x);
+  return p;
+}
+
+size_t moda_page_select_workspace_bytes(const moda_pages* x, const moda_shape* s) {
+  if (check_select(x, s) != MODA_OK) return 0;
+  return moda::select_workspace_bytes(select_dims(x, s));
+}
+
+moda_status moda_page_select(const void* Q, const void* Kbounds, const int32_t* page_table, const int32_t* lengths, int32_t* pages,
+                             int32_t keep, int32_t first, int32_t recent, void* workspace, size_t workspace_bytes, const moda_pages* x,
+                             const moda_shape* s, void* hip_stream) {
+  const moda_status st = check_select(x, s);
+  if (st != MODA_OK) return st;
+  if (keep < 1 || first < 0 || recent < 0 || (long long)first + recent > keep) return MODA_ERR_SHAPE;
+  if (s->B == 0) return MODA_OK;
+  if (!Q || !Kbounds || !page_table || !pages) return MODA_ERR_NULL;
+  for (const void* q : {Q, Kbounds, (const void*)workspace})
+    if (!aligned16(q)) return MODA_ERR_ALIGN;
+  if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(pages)) return MODA_ERR_ALIGN;
+  moda::SelectParams p = select_dims(x, s);
+  const size_t need = moda::select_workspace_bytes(p);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return MODA_ERR_WORKSPACE;
+  p.Q = Q; p.bounds = Kbounds; p.table = page_table; p.lengths = lengths; p.pages = pages;
+  p.keep = keep; p.first = first; p.recent = recent;
+  return launch_status(moda::launch_select(p, s->d, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+static moda_status check_decode_paged(const moda_pages* x, const moda_shape* s) {
+  const moda_status st = check_pages(x, s, kUsesHeads | kUsesT | kUsesDepth);
+  return st != MODA_OK ? st : check_length(x, s);
+}
+
+static moda::PagedParams paged_dims(const moda_pages* x, const moda_shape* s) {
+  moda::PagedParams p{};
+  p.B = s->B; p.Hq = s->Hq; p.Hk = s->Hk; p.T = s->T;
+  p.n_pages = x->n_pages; p.max_pages = x->max_pages; p.shift = shift_of(x);
+  p.depth_alloc = s->depth_alloc; p.depth_count = s->depth_count;
+  return p;
+}
+
+size_t moda_attn_decode_paged_workspace_bytes(const moda_pages* x, const moda_shape* s) {
+  if (check_decode_paged(x, s) != MODA_OK || s->B == 0) return 0;
+  return moda::decode_paged_workspace_bytes(paged_dims(x, s), s->d);
+}
+
+moda_status moda_attn_decode_paged(const void* Q, const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales,
+                                   const int32_t* page_table, const int32_t* lengths, const int32_t* selected, int32_t n_selected,
+                                   const void* Kdepth, const void* Vdepth, void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                                   const moda_pages* x, const moda_shape* s, void* hip_stream) {
+  moda_status st = check_decode_paged(x, s);
+  if (st != MODA_OK) return st;
+  if (selected && n_selected < 0) return MODA_ERR_SHAPE;
+  if (selected && (long long)n_selected * x->page_rows > 1ll << 30) return MODA_ERR_UNSUPPORTED;
+  if (s->B == 0) return MODA_OK;
+  if (!Q || !page_table || !O || !LSE) return MODA_ERR_NULL;
+  if (s->depth_count > 0 && (!Kdepth || !Vdepth)) return MODA_ERR_NULL;
+  if ((st = check_pools(Kpages, Vpages, Kscales, Vscales, x)) != MODA_OK) return st;
+  for (const void* q : {Q, Kdepth, Vdepth, (const void*)O, (const void*)LSE, (const void*)workspace})
+    if (!aligned16(q)) return MODA_ERR_ALIGN;
+  if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(selected)) return MODA_ERR_ALIGN;
+  moda::PagedParams p = paged_dims(x, s);
+  if (!workspace || workspace_bytes < moda::decode_paged_workspace_bytes(p, s->d)) return MODA_ERR_WORKSPACE;
+  p.Q = Q; p.K = (const char*)Kpages; p.V = (const char*)Vpages;
+  p.Ks = (const unsigned char*)Kscales; p.Vs = (const unsigned char*)Vscales;
+  p.table = page_table; p.lengths = lengths;
+  p.selected = selected; p.n_selected = n_selected;
+  p.Kd = (const char*)Kdepth; p.Vd = (const char*)Vdepth;
+  p.O = O; p.LSE = LSE;
+  p.scale = resolve_scale(s);
+  p.scale_log2 = p.scale * 1.4426950408889634f;
+  return launch_status(moda::launch_decode_paged(p, s->d, x->type == MODA_PAGES_MX8, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
 size_t moda_calibrate_mfma_operand_bytes(void) { return moda::calibrate_operand_bytes(); }
 size_t moda_calibrate_mfma_sink_bytes(int32_t workgroups) {
   return workgroups > 0 ? moda::calibrate_sink_bytes(workgroups) : 0;

@@ -1,0 +1,385 @@
+// Decoding step over a paged sequence cache: per new token one softmax over the rows of its sequence's pages, or of those that a list
+// names, and its depth slots.
+//
+// The formulas are those of moda_decode_shared.hip: (m, l, unnormalised O) of disjoint sets of rows merge exactly, so the rows are cut into
+// slices over workgroups, whose states go to the workspace in fp32, and a second kernel merges them.
+// The cut is made on the device, from the lengths themselves: a paged cache's table is as wide as the longest sequence may become, and a
+// cut by that bound would leave most workgroups without rows.  Slices are of one size for all sequences (least, good: see
+// launch_decode_paged), so that sequences of any lengths fill the chip evenly; every workgroup adds up the lengths and finds its slice.
+#include <algorithm>
+
+#include "moda_pages.h"
+
+namespace moda {
+
+constexpr int kPgWaves = 4;
+// Workgroups that the cut aims at: as many as there are compute units as long as their slices have `least` rows, twice that with `good`.
+constexpr int kPgFew = 256, kPgMany = 512;
+
+// ---------------------------------------------------------------- the cut
+// Rows of a sequence: of its cache, or of the places on its lists (whole pages: what a page holds is looked at later).
+__device__ __forceinline__ int paged_rows(const PagedParams& p, int b) {
+  return p.selected ? p.n_selected << p.shift : filled(p.lengths, b, p.T);
+}
+
+struct Slice {
+  int b;            // -1: no such slice
+  int begin, rows;  // its first row, and all rows of the sequence
+  int per;          // rows of a slice
+  int first, n;     // the sequence's first slice, and how many it has
+};
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) x += __shfl_xor(x, k);
+  return x;
+}
+// Slice s of all slices; a wave's lanes look at a sequence each.
+__device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lane) {
+  long long total = 0;  // (thousands of rows would do 32 bits, a large batch of long ones not: 16 bits at a time)
+  int rows = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
+    total += ((long long)wave_sum(rows >> 16) << 16) + wave_sum(rows & 0xffff);
+  }
+  auto whole = [&](long long n) { return (n + p.least - 1) / p.least * p.least; };
+  const long long few = whole((total * p.units + kPgFew - 1) / kPgFew), many = whole((total * p.units + kPgMany - 1) / kPgMany);
+  Slice r;
+  r.per = (int)max(min(few, max(many, (long long)p.good)), (long long)p.least);
+  r.b = -1;
+  int before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {  // (uniform)
+    if (p.B > 64) rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
+    const int n = b0 + lane < p.B ? max((int)(((unsigned)rows + r.per - 1) / (unsigned)r.per), 1) : 0;
+    int to = n;  // of this sequence and those before it
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+      const int x = __shfl_up(to, k);
+      if (lane >= k) to += x;
+    }
+    to += before;
+    const unsigned long long behind = __builtin_amdgcn_ballot_w64(to > s);
+    if (behind) {  // (uniform)
+      const int i = __builtin_ctzll(behind);
+      r.b = b0 + i;
+      r.rows = __builtin_amdgcn_readlane(rows, i);
+      r.n = __builtin_amdgcn_readlane(n, i);
+      r.first = __builtin_amdgcn_readlane(to, i) - r.n;
+      r.begin = (s - r.first) * r.per;
+      return r;
+    }
+    before = __builtin_amdgcn_readlane(to, 63);
+  }
+  return r;
+}
+
+// ---------------------------------------------------------------- pages
+// 64 pages of a sequence's list from page `base` on, one a lane: its number in the pool, and the rows that the sequence has in it.
+struct PageList {
+  const int* table;
+  const int* selected;  // or null
+  int n, len;           // pages on the list; rows of the sequence
+  int base, id, count;
+  __device__ __forceinline__ void init(const PagedParams& p, int b, int g) {
+    len = filled(p.lengths, b, p.T);
+    n = (len + (1 << p.shift) - 1) >> p.shift;
+    table = p.table + (size_t)b * p.max_pages;
+    selected = p.selected ? p.selected + ((size_t)b * p.Hk + g) * p.n_selected : nullptr;
+  }
+  __device__ __forceinline__ void load(const PagedParams& p, int from, int lane) {
+    base = from;
+    const int i = from + lane;
+    int page = i;
+    if (selected) page = i < p.n_selected ? selected[i] : -1;
+    const bool there = page >= 0 && page < n;
+    const int at = there ? page_at(table, page, p.n_pages) : -1;
+    id = max(at, 0);
+    count = at < 0 ? 0 : min(len - (page << p.shift), 1 << p.shift);
+  }
+};
+
+// ---------------------------------------------------------------- rows on the vector ALUs
+// A lane owns CPL channels (16 bytes of a cached row), D / CPL lanes a row; a wave takes kU batches of adjacent rows at a time.
+template <int D, int GT, int CPL>
+struct RowState {
+  static constexpr int LPR = D / CPL, RPS = 64 / LPR, kU = 4;
+  uint32_t q[GT][CPL / 2];
+  float m[GT], l[GT], o[GT][CPL];
+  template <class Query>
+  __device__ __forceinline__ void init(Query&& query, int nh, int l16) {
+#pragma unroll
+    for (int j = 0; j < GT; ++j) {
+#pragma unroll
+      for (int k = 0; k < CPL / 8; ++k) *(u32x4*)&q[j][k * 4] = *(const u32x4*)(query(min(j, nh - 1)) + l16 * CPL * 2 + k * 16);
+      m[j] = -INFINITY;
+      l[j] = 0.f;
+#pragma unroll
+      for (int k = 0; k < CPL; ++k) o[j][k] = 0.f;
+    }
+  }
+  // kU batches: key(u, i) = channels 2 i, 2 i + 1 as packed bf16, value(u, i) = the same of V as two floats; row rg of batch u counts if rg < left[u].
+  template <class Key, class Value>
+  __device__ __forceinline__ void fold(Key&& key, Value&& value, const int (&left)[kU], int rg, float c2) {
+    float sc[GT][kU];
+#pragma unroll
+    for (int j = 0; j < GT; ++j)
+#pragma unroll
+      for (int u = 0; u < kU; ++u) sc[j][u] = 0.f;
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int i = 0; i < CPL / 2; ++i) {
+        const uint32_t k = key(u, i);
+#pragma unroll
+        for (int j = 0; j < GT; ++j) sc[j][u] = dot2_bf16(q[j][i], k, sc[j][u]);
+      }
+#pragma unroll
+    for (int j = 0; j < GT; ++j) {
+      float mn = m[j];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        float a = sc[j][u];
+        a += dpp_mov<0xB1>(a);
+        a += dpp_mov<0x4E>(a);
+        if (LPR >= 8) a += dpp_mov<0x141>(a);
+        if (LPR >= 16) a += dpp_mov<0x140>(a);
+        sc[j][u] = rg < left[u] ? a : -INFINITY;
+        mn = fmaxf(mn, sc[j][u]);
+      }
+      // (mn is -inf only while every score so far was, or was NaN, which stays NaN; with reference 0 the others weigh nothing)
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      const float al = fast_exp2((m[j] - ref) * c2);
+      m[j] = mn;
+      l[j] *= al;
+#pragma unroll
+      for (int k = 0; k < CPL; ++k) o[j][k] *= al;
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        sc[j][u] = fast_exp2((sc[j][u] - ref) * c2);
+        l[j] += sc[j][u];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int i = 0; i < CPL / 2; ++i) {
+        const f32x2 v = value(u, i);
+#pragma unroll
+        for (int j = 0; j < GT; ++j) {
+          o[j][2 * i] += sc[j][u] * v[0];
+          o[j][2 * i + 1] += sc[j][u] * v[1];
+        }
+      }
+  }
+};
+
+// A batch of rows in flight: 16 bytes of K and of V per lane, and the scales of 8-bit rows.
+template <int kU, bool MX>
+struct RowBatch {
+  u32x4 k[kU], v[kU];
+  unsigned ks[MX ? kU : 1], vs[MX ? kU : 1];
+  int left[kU];
+};
+
+template <int D, int GT, bool MX>
+__global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(PagedParams p) {
+  constexpr int CPL = MX ? 16 : 8, LPR = D / CPL, RPS = 64 / LPR, RB = D * 2, CB = MX ? D : RB, SB = D / kBlock;
+  using State = RowState<D, GT, CPL>;
+  constexpr int kU = State::kU, STEP = kPgWaves * kU * RPS;
+  __shared__ __attribute__((aligned(16))) float red[kPgWaves * GT * (D + 2)];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane % LPR, rg = lane / LPR;
+  const float c2 = p.scale_log2;
+  const int unit = blockIdx.x % p.units, s = blockIdx.x / p.units;
+  const Slice x = find_slice(p, s, lane);
+  if (x.b < 0) return;  // (uniform)
+  const int b = x.b, G = p.Hq / p.Hk, g = unit % p.Hk, gc = unit / p.Hk;
+  const int nh = min(GT, G - gc * GT);
+  const size_t bh = (size_t)b * p.Hq + g * G + gc * GT;
+  if (unit == 0 && s == x.first && tid == 0) {
+    p.ws_deal[2 * b] = x.first;
+    p.ws_deal[2 * b + 1] = x.n;
+  }
+  State st;
+  st.init([&](int j) { return (const char*)p.Q + (bh + j) * RB; }, nh, l16);
+  const int end = min(x.rows, x.begin + x.per);
+  if (x.begin < end) {  // (uniform)
+    PageList list;
+    list.init(p, b, g);
+    list.load(p, x.begin >> p.shift, lane);
+    using Batch = RowBatch<kU, MX>;
+    auto issue = [&](int row, Batch& r) {
+      if (((row + kU * RPS - 1) >> p.shift) - list.base >= 64) list.load(p, row >> p.shift, lane);  // (uniform)
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int at = row + u * RPS, i = (at >> p.shift) - list.base, slot = at & ((1 << p.shift) - 1);
+        const int id = __builtin_amdgcn_readlane(list.id, i), count = __builtin_amdgcn_readlane(list.count, i);
+        const size_t row0 = ((size_t)id * p.Hk + g) << p.shift;
+        const __amdgpu_buffer_rsrc_t kb = rows_buffer(p.K + row0 * CB, count * CB), vb = rows_buffer(p.V + row0 * CB, count * CB);
+        r.k[u] = __builtin_amdgcn_raw_buffer_load_b128(kb, (slot + rg) * CB + l16 * 16, 0, 2);
+        r.v[u] = __builtin_amdgcn_raw_buffer_load_b128(vb, (slot + rg) * CB + l16 * 16, 0, 2);
+        if (MX) {
+          const __amdgpu_buffer_rsrc_t ksb = rows_buffer(p.Ks + row0 * SB, count * SB), vsb = rows_buffer(p.Vs + row0 * SB, count * SB);
+          r.ks[u] = __builtin_amdgcn_raw_buffer_load_b8(ksb, (slot + rg) * SB + l16 * CPL / kBlock, 0, 0);
+          r.vs[u] = __builtin_amdgcn_raw_buffer_load_b8(vsb, (slot + rg) * SB + l16 * CPL / kBlock, 0, 0);
+        }
+        r.left[u] = count - slot;
+      }
+    };
+    const int row0 = x.begin + wave * kU * RPS;
+    Batch next;
+    issue(row0, next);
+    for (int base = x.begin; base < end; base += STEP) {  // (uniform)
+      const Batch r = next;
+      if (base + STEP < end) issue(row0 + (base - x.begin) + STEP, next);  // (uniform)
+      if constexpr (MX) {
+        st.fold([&](int u, int i) { return i % 2 ? codes_bf16<true>(r.k[u][i / 2], scale_of(r.ks[u])) : codes_bf16<false>(r.k[u][i / 2], scale_of(r.ks[u])); },
+                [&](int u, int i) { return i % 2 ? codes_f32<true>(r.v[u][i / 2], scale_of(r.vs[u])) : codes_f32<false>(r.v[u][i / 2], scale_of(r.vs[u])); },
+                r.left, rg, c2);
+      } else {
+        st.fold([&](int u, int i) { return r.k[u][i]; }, [&](int u, int i) { return (f32x2){bf16_lo(r.v[u][i]), bf16_hi(r.v[u][i])}; }, r.left, rg, c2);
+      }
+    }
+  }
+  if (s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice
+    const size_t at = ((size_t)b * p.Hk + g) * p.depth_alloc * RB;
+    const __amdgpu_buffer_rsrc_t kb = rows_buffer(p.Kd + at, p.depth_count * RB), vb = rows_buffer(p.Vd + at, p.depth_count * RB);
+    constexpr int W = CPL / 8;  // 16-byte pieces of a lane's channels
+    for (int row = wave * kU * RPS; row < p.depth_count; row += STEP) {
+      u32x4 k[kU][W], v[kU][W];
+      int left[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          k[u][w] = __builtin_amdgcn_raw_buffer_load_b128(kb, (row + u * RPS + rg) * RB + l16 * CPL * 2 + w * 16, 0, 0);
+          v[u][w] = __builtin_amdgcn_raw_buffer_load_b128(vb, (row + u * RPS + rg) * RB + l16 * CPL * 2 + w * 16, 0, 0);
+        }
+        left[u] = p.depth_count - row - u * RPS;
+      }
+      st.fold([&](int u, int i) { return k[u][i / 4][i % 4]; }, [&](int u, int i) { return (f32x2){bf16_lo(v[u][i / 4][i % 4]), bf16_hi(v[u][i / 4][i % 4])}; },
+              left, rg, c2);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < GT; ++j) fold_groups<D>(st.m[j], st.l[j], st.o[j], c2, lane, red + (wave * GT + j) * (D + 2));
+  __syncthreads();
+  const size_t to = (size_t)s * p.Hq + g * G + gc * GT;
+  for (int t = tid; t < nh * D; t += kPgWaves * 64) {
+    const int j = t / D, ch = t % D;
+    float o;
+    const f32x2 ml = fold_rows<D, GT, kPgWaves>(red, j, ch, c2, o);
+    p.ws_o[to * D + t] = o;
+    if (ch == 0) *(f32x2*)(p.ws_ml + (to + j) * 2) = ml;
+  }
+}
+
+// ---------------------------------------------------------------- outputs
+// `by` slices of a head at a time, D / 4 threads each (four channels a thread), 1024 / D such teams in a workgroup.
+template <int D>
+__global__ __launch_bounds__(256) void moda_paged_finish_kernel(PagedParams p, int by) {
+  constexpr int kTeam = D / 4, kTeams = 256 / kTeam;
+  __shared__ __attribute__((aligned(16))) float red[kTeams][D + 4];
+  const float c2 = p.scale_log2;
+  const int tid = threadIdx.x;
+  // (a state whose scores are all -inf is empty: reference -inf, weight zero)
+  auto factor = [&](float m, float ref) { return m == -INFINITY ? 0.f : fast_exp2((m - ref) * c2); };
+  const int team = tid / kTeam, ch = tid % kTeam * 4, part = team % by;
+  const long long bh = (long long)blockIdx.x * (kTeams / by) + team / by, heads = (long long)p.B * p.Hq;
+  const int row = (int)min(bh, heads - 1), b = row / p.Hq, h = row % p.Hq;
+  const int first = p.ws_deal[2 * b], n = p.ws_deal[2 * b + 1];
+  float mm = -INFINITY, ll = 0.f;
+  f32x4 oo = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kU = 4;
+  for (int s0 = part; s0 < n; s0 += kU * by) {
+    f32x2 st[kU];
+    f32x4 o[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const size_t i = (size_t)(first + min(s0 + u * by, n - 1)) * p.Hq + h;
+      st[u] = *(const f32x2*)(p.ws_ml + i * 2);
+      o[u] = *(const f32x4*)(p.ws_o + i * D + ch);
+    }
+    float mn = mm;
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (s0 + u * by < n) mn = fmaxf(mn, st[u][0]);
+    const float al = factor(mm, mn);
+    mm = mn;
+    ll *= al;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) oo[j] *= al;
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (s0 + u * by < n) {
+        const float f = factor(st[u][0], mm);
+        ll += f * st[u][1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) oo[j] += f * o[u][j];
+      }
+  }
+  if (by > 1) {  // (uniform)
+    *(f32x4*)&red[team][ch] = oo;
+    if (ch == 0) *(f32x2*)&red[team][D] = (f32x2){mm, ll};
+    __syncthreads();
+    if (part > 0) return;
+    const float m0 = mm;
+    for (int k = 1; k < by; ++k) mm = fmaxf(mm, red[team + k][D]);
+    const float f0 = factor(m0, mm);
+    ll *= f0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) oo[j] *= f0;
+    for (int k = 1; k < by; ++k) {
+      const float f = factor(red[team + k][D], mm);
+      ll += f * red[team + k][D + 1];
+      const f32x4 x = *(const f32x4*)&red[team + k][ch];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) oo[j] += f * x[j];
+    }
+  }
+  if (bh >= heads) return;
+  const bool none = ll == 0.f;  // nothing seen, or nothing that has weight
+  const float inv = none ? 0.f : 1.f / ll;
+  *(u32x2*)((__bf16*)p.O + bh * D + ch) = none ? (u32x2){0u, 0u} : (u32x2){pack_bf16(oo[0] * inv, oo[1] * inv), pack_bf16(oo[2] * inv, oo[3] * inv)};
+  if (ch == 0) p.LSE[bh] = none ? -INFINITY : mm * p.scale + __logf(ll);
+}
+
+// ---------------------------------------------------------------- host side
+static void plan(PagedParams& p, int d, bool mx) {
+  const int G = p.Hq / p.Hk;
+  p.heads_per = G <= 2 ? G : 4;
+  p.units = p.Hk * ((G + p.heads_per - 1) / p.heads_per);
+  p.least = kPgWaves * 4 * 64 * (mx ? 16 : 8) / d;  // what the waves take at a time
+  p.good = std::max(256, p.least);
+  // Slices of one size, `least` or more, and one more of every sequence: find_slice's sizes make no more.
+  p.n_slices = p.B + kPgMany / p.units;
+}
+
+size_t decode_paged_workspace_bytes(const PagedParams& dims, int d) {
+  // (whichever way the rows are read: one head per workgroup makes the fewest units)
+  const size_t slices = (size_t)dims.B + kPgMany / dims.Hk;
+  return (slices * dims.Hq * (d + 2) + 2 * (size_t)dims.B) * sizeof(float);
+}
+
+template <int D, bool MX>
+static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
+  const long long blocks = (long long)p.units * p.n_slices, heads = (long long)p.B * p.Hq;
+  constexpr int teams = 1024 / D;
+  int by = 1;  // teams that share a head's slices, so that each folds about four of them at a time
+  while (by < teams && (long long)by * 4 * p.B < p.n_slices) by *= 2;
+  const long long finish_blocks = (heads + teams / by - 1) / (teams / by);
+  if (!grid_ok(blocks, kPgWaves * 64) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
+  auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX> : moda_paged_slices_kernel<D, 4, MX>;
+  const hipError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kPgWaves * 64), stream, p);
+  if (e != hipSuccess) return e;
+  return launch_kernel(moda_paged_finish_kernel<D>, dim3((unsigned)finish_blocks), dim3(256), stream, p, by);
+}
+
+hipError_t launch_decode_paged(PagedParams p, int d, bool mx, void* workspace, hipStream_t stream) {
+  plan(p, d, mx);
+  p.ws_o = (float*)workspace;
+  p.ws_ml = p.ws_o + (size_t)p.n_slices * p.Hq * d;
+  p.ws_deal = (int*)(p.ws_ml + (size_t)p.n_slices * p.Hq * 2);
+  if (d == 128) return mx ? launch_d<128, true>(p, stream) : launch_d<128, false>(p, stream);
+  return mx ? launch_d<64, true>(p, stream) : launch_d<64, false>(p, stream);
+}
+
+}  // namespace moda

@@ -53,10 +53,6 @@ struct Rows {
   int n2;
 };
 
-__device__ __forceinline__ int filled(const int* lengths, int i, int most) {
-  return lengths ? min(max(lengths[i], 0), most) : most;
-}
-
 // ---------------------------------------------------------------- rows on the vector ALUs
 // A lane owns 8 channels, d/8 lanes a row; a wave takes kU batches of 64 / (d/8) rows at a time, the next ones in
 // flight, and raises its reference once for them.  query(j) = the address of query j of GT (from nh on the last one repeats and is
@@ -154,24 +150,7 @@ __device__ __forceinline__ void walk_rows(const Rows& x, Query&& query, int nh, 
   __syncthreads();
 }
 
-// (reference, normaliser) of query j's waves, and channel ch's sum.
-template <int D, int GT, int WAVES>
-__device__ __forceinline__ f32x2 fold_rows(const float* red, int j, int ch, float c2, float& oo) {
-  float mm = -INFINITY, ll = 0.f;
-  oo = 0.f;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, red[(w * GT + j) * (D + 2) + D]);
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const float* x = red + (w * GT + j) * (D + 2);
-    const float f = x[D] == -INFINITY ? 0.f : fast_exp2((x[D] - mm) * c2);
-    ll += f * x[D + 1];
-    oo += f * x[ch];
-  }
-  return (f32x2){mm, ll};
-}
-
-// ... and the queries' states to o_out, ml_out.
+// The queries' states of walk_rows, waves folded, to o_out, ml_out.
 template <int D, int GT, class Query>
 __device__ __forceinline__ void read_rows(const Rows& x, Query&& query, int nh, float c2, float* o_out, float* ml_out, float* scores,
                                           size_t score_step, float* red) {

@@ -135,6 +135,71 @@ struct EvictParams {
 size_t evict_workspace_bytes(int B, int Hk, int T, int keep);
 hipError_t launch_evict(const EvictParams& p, void* workspace, hipStream_t stream);
 
+// Rows into and out of a paged sequence cache (moda_page_rows.hip).  Pages of 1 << shift rows.
+struct PageRowsParams {
+  const char* K;  // append: new rows, [B, Hk, T, row_bytes]
+  const char* V;
+  char* K_out;  // read: the same
+  char* V_out;
+  const int* table;    // [B, max_pages]
+  const int* lengths;  // [B] or null
+  const int* counts;   // [B] or null (append)
+  char* Kp;            // [n_pages, Hk, rows, d] bf16 or codes
+  char* Vp;
+  unsigned char* Ks;  // [n_pages, Hk, rows, d / 32]
+  unsigned char* Vs;
+  char* bounds;  // [n_pages, Hk, 2, d] bf16 or null (append)
+  int B, Hk, T, first;
+  int n_pages, max_pages, shift;
+};
+hipError_t launch_page_append(const PageRowsParams& p, int d, bool mx, hipStream_t stream);
+hipError_t launch_page_read(const PageRowsParams& p, int d, bool mx, hipStream_t stream);
+
+// The choice of pages by their bounds (moda_page_select.hip).
+struct SelectParams {
+  const void* Q;       // [B, Hq, d]
+  const void* bounds;  // [n_pages, Hk, 2, d]
+  const int* table;    // [B, max_pages]
+  const int* lengths;  // [B] or null
+  int* pages;          // [B, Hk, keep]
+  unsigned long long* keys;  // workspace: [B, Hk, cols], scores as integers of the same order
+  int cols;
+  int B, Hq, Hk, T;
+  int n_pages, max_pages, shift;
+  int keep, first, recent;
+};
+size_t select_workspace_bytes(const SelectParams& p);
+hipError_t launch_select(SelectParams p, int d, void* workspace, hipStream_t stream);
+
+// Decoding step over a paged cache (moda_decode_paged.hip).
+struct PagedParams {
+  const void* Q;  // [B, Hq, d]
+  const char* K;  // [n_pages, Hk, rows, d] bf16 or codes
+  const char* V;
+  const unsigned char* Ks;  // [n_pages, Hk, rows, d / 32], 8-bit pages only
+  const unsigned char* Vs;
+  const int* table;     // [B, max_pages]
+  const int* lengths;   // [B] or null
+  const int* selected;  // [B, Hk, n_selected] or null
+  const char* Kd;       // [B, Hk, depth_alloc, d]
+  const char* Vd;
+  void* O;
+  float* LSE;
+  float* ws_o;   // [slices, Hq, d]: unnormalised outputs
+  float* ws_ml;  // [slices, Hq, 2]: references (logits before the scale) and normalisers
+  int* ws_deal;  // [B, 2]: a sequence's first slice and how many it has
+  int B, Hq, Hk, T;
+  int n_pages, max_pages, shift;
+  int n_selected;
+  int depth_alloc, depth_count;
+  int units, heads_per;  // workgroups of a slice; query heads of one
+  int least, good;       // rows that slices are multiples of; rows of one once the chip is full
+  int n_slices;          // most slices of all sequences together
+  float scale, scale_log2;
+};
+size_t decode_paged_workspace_bytes(const PagedParams& p, int d);
+hipError_t launch_decode_paged(PagedParams p, int d, bool mx, void* workspace, hipStream_t stream);
+
 // Matrix-pipe calibration kernel (moda_calibrate.hip).
 size_t calibrate_operand_bytes();
 size_t calibrate_sink_bytes(int workgroups);
