@@ -35,6 +35,12 @@ decltype(&moda_attn_weights) g_weights;
 decltype(&moda_attn_weights_workspace_bytes) g_weights_bytes;
 decltype(&moda_cache_evict) g_evict;
 decltype(&moda_cache_evict_workspace_bytes) g_evict_bytes;
+decltype(&moda_page_append) g_page_append;
+decltype(&moda_page_read) g_page_read;
+decltype(&moda_page_select) g_page_select;
+decltype(&moda_page_select_workspace_bytes) g_page_select_bytes;
+decltype(&moda_attn_decode_paged) g_paged;
+decltype(&moda_attn_decode_paged_workspace_bytes) g_paged_bytes;
 
 // An argument that must be a plain strided tensor in device memory, or None.
 struct Arg {
@@ -378,6 +384,160 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// The pools, scales and table of a paged cache for sequences on `dev`; fills `x`.
+struct Pages {
+  const Arg k, v, table, ks, vs;
+  int64_t n = 0, Hk = 0, R = 0, d = 0, cols = 0;
+  Pages(PyObject* kp, PyObject* vp, PyObject* t, PyObject* kscales, PyObject* vscales) : k(kp), v(vp), table(t), ks(kscales), vs(vscales) {}
+  bool read(int64_t B, c10::Device dev, moda_pages& x) {
+    for (const Arg* a : {&k, &v, &table, &ks, &vs})
+      if (!a->ok) return false;
+    if (!k || !v || !table || k->dim() != 4 || table->dim() != 2 || !fits(*k.t) || !fits(*table.t)) return false;
+    n = k->size(0); Hk = k->size(1); R = k->size(2); d = k->size(3); cols = table->size(1);
+    const auto dt = k->scalar_type();
+    const bool mx = dt == at::kFloat8_e4m3fn;
+    if ((!mx && dt != at::kBFloat16) || mx != (bool)ks || mx != (bool)vs) return false;
+    x.n_pages = n; x.page_rows = R; x.max_pages = cols; x.type = mx ? MODA_PAGES_MX8 : MODA_PAGES_BF16;
+    return k.is(dt, dev, {n, Hk, R, d}) && v.is(dt, dev, {n, Hk, R, d}) && ks.is(at::kByte, dev, {n, Hk, R, d / 32}) &&
+           vs.is(at::kByte, dev, {n, Hk, R, d / 32}) && table.is(at::kInt, dev, {B, cols});
+  }
+};
+
+// The rows that lengths may reach: an int, or (None) all that the table has.
+bool bound_arg(PyObject* o, int64_t cols, int64_t rows, int32_t& T) { return int_arg(o, cols * rows, T); }
+
+void plain_shape(moda_shape& s, int64_t B, int64_t Hq, int64_t Hk, int64_t T, int64_t d) {
+  s.B = B; s.Hq = Hq; s.Hk = Hk; s.T = T; s.d = d;
+  s.depth_alloc = 0; s.depth_count = 0; s.causal = 1; s.scale = 0.f; s.dtype = MODA_BF16;
+}
+
+// (K, V, Kpages, Vpages, page_table, lengths, counts, Kscales, Vscales, Kbounds); returns True
+PyObject* page_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(10);
+  const Arg k(a[0]), v(a[1]), lens(a[5]), counts(a[6]), bounds(a[9]);
+  Pages c(a[2], a[3], a[4], a[7], a[8]);
+  for (const Arg* x : {&k, &v, &lens, &counts, &bounds})
+    if (!x->ok) Py_RETURN_NONE;
+  if (!g_page_append || !k || !v || k->dim() != 4 || !fits(*k.t)) Py_RETURN_NONE;
+  const int64_t B = k->size(0), Hk = k->size(1), T = k->size(2), d = k->size(3);
+  const auto dev = k->device();
+  moda_pages x;
+  moda_shape s;
+  if (!c.read(B, dev, x) || c.Hk != Hk || c.d != d || !k.is(at::kBFloat16, dev, {B, Hk, T, d}) || !v.is(at::kBFloat16, dev, {B, Hk, T, d}) ||
+      !lens.is(at::kInt, dev, {B}) || !counts.is(at::kInt, dev, {B}) || !bounds.is(at::kBFloat16, dev, {c.n, Hk, 2, d}))
+    Py_RETURN_NONE;
+  plain_shape(s, B, Hk, Hk, T, d);
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {k.ptr(), v.ptr(), c.table.ptr(), lens.ptr(), counts.ptr(), c.k.ptr(), c.v.ptr(), c.ks.ptr(), c.vs.ptr(), bounds.ptr()};
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_page_append(p[0], p[1], (const int32_t*)p[2], (const int32_t*)p[3], (const int32_t*)p[4], p[5], p[6], p[7], p[8], p[9], &x, &s, st);
+  });
+  if (rc == MODA_OK) Py_RETURN_TRUE;
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// (Kpages, Vpages, page_table, lengths, first, Kscales, Vscales, K, V); returns True
+PyObject* page_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(9);
+  const Arg lens(a[3]), k(a[7]), v(a[8]);
+  Pages c(a[0], a[1], a[2], a[5], a[6]);
+  int32_t first;
+  if (!lens.ok || !k.ok || !v.ok || !g_page_read || !k || !v || k->dim() != 4 || !fits(*k.t) || a[4] == Py_None || !int_arg(a[4], 0, first))
+    Py_RETURN_NONE;
+  const int64_t B = k->size(0), Hk = k->size(1), T = k->size(2), d = k->size(3);
+  const auto dev = k->device();
+  moda_pages x;
+  moda_shape s;
+  if (!c.read(B, dev, x) || c.Hk != Hk || c.d != d || !k.is(at::kBFloat16, dev, {B, Hk, T, d}) || !v.is(at::kBFloat16, dev, {B, Hk, T, d}) ||
+      !lens.is(at::kInt, dev, {B}))
+    Py_RETURN_NONE;
+  plain_shape(s, B, Hk, Hk, T, d);
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {c.k.ptr(), c.v.ptr(), c.ks.ptr(), c.vs.ptr(), c.table.ptr(), lens.ptr(), k.ptr(), v.ptr()};
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_page_read(p[0], p[1], p[2], p[3], (const int32_t*)p[4], (const int32_t*)p[5], p[6], p[7], first, &x, &s, st);
+  });
+  if (rc == MODA_OK) Py_RETURN_TRUE;
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// (Q, Kbounds, page_table, keep, page_rows, lengths, first, recent, T, out, workspace); returns True
+PyObject* page_select(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(11);
+  const Arg q(a[0]), bounds(a[1]), table(a[2]), lens(a[5]), out(a[9]), ws(a[10]);
+  for (const Arg* x : {&q, &bounds, &table, &lens, &out, &ws})
+    if (!x->ok) Py_RETURN_NONE;
+  if (!g_page_select || !q || !bounds || !table || !out || q->dim() != 3 || bounds->dim() != 4 || table->dim() != 2 || !fits(*q.t) ||
+      !fits(*bounds.t) || !fits(*table.t))
+    Py_RETURN_NONE;
+  for (int i : {3, 4, 6, 7})
+    if (a[i] == Py_None) Py_RETURN_NONE;
+  const int64_t B = q->size(0), Hq = q->size(1), d = q->size(2), n = bounds->size(0), Hk = bounds->size(1), cols = table->size(1);
+  const auto dev = q->device();
+  moda_pages x;
+  moda_shape s;
+  int32_t keep, first, recent;
+  if (!int_arg(a[3], 0, keep) || !int_arg(a[4], 0, x.page_rows) || !int_arg(a[6], 0, first) || !int_arg(a[7], 0, recent)) Py_RETURN_NONE;
+  plain_shape(s, B, Hq, Hk, 0, d);
+  x.n_pages = n; x.max_pages = cols; x.type = MODA_PAGES_BF16;
+  if (!bound_arg(a[8], cols, x.page_rows, s.T) || !q.is(at::kBFloat16, dev, {B, Hq, d}) || !bounds.is(at::kBFloat16, dev, {n, Hk, 2, d}) ||
+      !table.is(at::kInt, dev, {B, cols}) || !lens.is(at::kInt, dev, {B}) || !out.is(at::kInt, dev, {B, Hk, keep}))
+    Py_RETURN_NONE;
+  at::Tensor w;
+  if (!workspace_arg(ws, dev, [&] { return g_page_select_bytes(&x, &s); }, w)) Py_RETURN_NONE;
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {q.ptr(), bounds.ptr(), table.ptr(), lens.ptr(), out.ptr(), w.data_ptr()};
+  const size_t ws_bytes = bytes_of(w);
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_page_select(p[0], p[1], (const int32_t*)p[2], (const int32_t*)p[3], (int32_t*)p[4], keep, first, recent, p[5], ws_bytes, &x, &s, st);
+  });
+  if (rc == MODA_OK) Py_RETURN_TRUE;
+  return PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// (Q, Kpages, Vpages, page_table, Kdepth, Vdepth, lengths, selected, Kscales, Vscales, T, depth_count, scale, out, lse, workspace);
+// returns (out, lse)
+PyObject* paged(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  MODA_TAKES(16);
+  const Arg q(a[0]), kd(a[4]), vd(a[5]), lens(a[6]), sel(a[7]), out(a[13]), lse(a[14]), ws(a[15]);
+  Pages c(a[1], a[2], a[3], a[8], a[9]);
+  for (const Arg* x : {&q, &kd, &vd, &lens, &sel, &out, &lse, &ws})
+    if (!x->ok) Py_RETURN_NONE;
+  if (!g_paged || !q || q->dim() != 3 || !fits(*q.t) || (kd && (kd->dim() != 4 || !fits(*kd.t))) || (sel && (sel->dim() != 3 || !fits(*sel.t))))
+    Py_RETURN_NONE;
+  const int64_t B = q->size(0), Hq = q->size(1), d = q->size(2), La = kd ? kd->size(2) : 0, ns = sel ? sel->size(2) : 0;
+  const auto dev = q->device();
+  moda_pages x;
+  moda_shape s;
+  if (!c.read(B, dev, x) || c.d != d || (sel && ns == 0)) Py_RETURN_NONE;
+  plain_shape(s, B, Hq, c.Hk, 0, d);
+  s.depth_alloc = La;
+  if (!bound_arg(a[10], c.cols, c.R, s.T) || !int_arg(a[11], La, s.depth_count) || !scale_arg(a[12], s.scale) || !q.is(at::kBFloat16, dev, {B, Hq, d}) ||
+      !kd.is(at::kBFloat16, dev, {B, c.Hk, La, d}) || !vd.is(at::kBFloat16, dev, {B, c.Hk, La, d}) || !lens.is(at::kInt, dev, {B}) ||
+      !sel.is(at::kInt, dev, {B, c.Hk, ns}) || !out.is(at::kBFloat16, dev, {B, Hq, d}) || !lse.is(at::kFloat, dev, {B, Hq}))
+    Py_RETURN_NONE;
+  at::Tensor w;
+  if (!workspace_arg(ws, dev, [&] { return g_paged_bytes(&x, &s); }, w)) Py_RETURN_NONE;
+  const at::Tensor r[2] = {out ? *out.t : at::empty_like(*q.t), lse ? *lse.t : at::empty({B, Hq}, q->options().dtype(at::kFloat))};
+  const c10::DeviceGuard guard(dev);
+  void* const p[] = {q.ptr(), c.k.ptr(), c.v.ptr(), c.ks.ptr(), c.vs.ptr(), c.table.ptr(), lens.ptr(), sel.ptr(), kd.ptr(), vd.ptr(),
+                     r[0].data_ptr(), r[1].data_ptr(), w.data_ptr()};
+  const size_t ws_bytes = bytes_of(w);
+  void* const st = stream_of(dev);
+  const moda_status rc = unlocked([&] {
+    return g_paged(p[0], p[1], p[2], p[3], p[4], (const int32_t*)p[5], (const int32_t*)p[6], (const int32_t*)p[7], (int32_t)ns, p[8], p[9], p[10],
+                   (float*)p[11], p[12], ws_bytes, &x, &s, st);
+  });
+  return rc == MODA_OK ? tuple_of(r) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
 // n addresses, none of them null; false with the exception set.
 bool addresses(PyObject* const* a, Py_ssize_t nargs, void** p, Py_ssize_t n) {
   if (nargs != n) {
@@ -416,10 +576,23 @@ PyObject* init_cache(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   g_evict_bytes = (decltype(g_evict_bytes))p[5];
   Py_RETURN_NONE;
 }
+// (... of the six of a paged cache)
+PyObject* init_pages(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  void* p[6];
+  if (!addresses(a, nargs, p, 6)) return nullptr;
+  g_page_append = (decltype(g_page_append))p[0];
+  g_page_read = (decltype(g_page_read))p[1];
+  g_page_select = (decltype(g_page_select))p[2];
+  g_page_select_bytes = (decltype(g_page_select_bytes))p[3];
+  g_paged = (decltype(g_paged))p[4];
+  g_paged_bytes = (decltype(g_paged_bytes))p[5];
+  Py_RETURN_NONE;
+}
 
 #define MODA_METHOD(f) {#f, (PyCFunction)(void (*)())f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MODA_METHOD(init), MODA_METHOD(fwd), MODA_METHOD(bwd), MODA_METHOD(decode), MODA_METHOD(append),
                          MODA_METHOD(init_cache), MODA_METHOD(shared), MODA_METHOD(weights), MODA_METHOD(evict),
+                         MODA_METHOD(init_pages), MODA_METHOD(page_append), MODA_METHOD(page_read), MODA_METHOD(page_select), MODA_METHOD(paged),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "moda_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -4,8 +4,8 @@ Argument marshalling only: torch tensors supply device memory and the stream;
 every step of the attention runs in the HIP kernels of libmoda.so.  There is no
 fallback: if the library is missing or a call is rejected, an exception is raised.
 
-Plain valid calls of moda_attn_fwd, moda_attn_bwd, moda_attn_decode, moda_depth_append and of the calls on a shared or
-bounded cache are marshalled by moda_torch.so (bind_csrc/moda_torch.cpp); whatever it declines comes back as None and is taken here,
+Plain valid calls of moda_attn_fwd, moda_attn_bwd, moda_attn_decode, moda_depth_append and of the calls on a shared,
+bounded or paged cache are marshalled by moda_torch.so (bind_csrc/moda_torch.cpp); whatever it declines comes back as None and is taken here,
 through ctypes, with the same checks and an exception for the one that fails.
 """
 import ctypes
@@ -159,6 +159,9 @@ def _native():
         m.init_cache(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                        (L.moda_attn_decode_shared, L.moda_attn_decode_shared_workspace_bytes, L.moda_attn_weights,
                         L.moda_attn_weights_workspace_bytes, L.moda_cache_evict, L.moda_cache_evict_workspace_bytes)))
+        m.init_pages(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                       (L.moda_page_append, L.moda_page_read, L.moda_page_select, L.moda_page_select_workspace_bytes,
+                        L.moda_attn_decode_paged, L.moda_attn_decode_paged_workspace_bytes)))
         _native_module = m
     return _native_module
 
@@ -564,6 +567,10 @@ def moda_page_append(K, V, Kpages, Vpages, page_table, lengths=None, counts=None
     (int32): the page of each page_rows rows of a sequence, -1: none.  lengths [B] (int32; None: T): the rows of each sequence after
     the call, of which the last min(T, counts [B], length) are the new ones.  Kbounds [n_pages,Hk,2,d] (bf16): the least and
     largest key channels of every page written are kept there.  Returns Kpages, Vpages."""
+    r = (_native_module or _native()).page_append(K, V, Kpages, Vpages, page_table, lengths, counts, Kscales, Vscales, Kbounds)
+    if r is not None:
+        _outputs(r)
+        return Kpages, Vpages
     B, Hk, T, d = K.shape
     dev = K.device
     x = _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, dev)
@@ -586,6 +593,11 @@ def moda_page_read(Kpages, Vpages, page_table, lengths=None, first=0, T=None, Ks
     pages hold them.  T None: that of `out`, else all rows that the table has from `first` on.  Rows from a sequence's
     length on (lengths [B]; None: all are there) and those of missing pages are left as they were in out = (K, V); without
     `out` they are zero."""
+    if out is not None and T is None:
+        r = (_native_module or _native()).page_read(Kpages, Vpages, page_table, lengths, first, Kscales, Vscales, *out)
+        if r is not None:
+            _outputs(r)
+            return out[0], out[1]
     B, dev = page_table.shape[0], Kpages.device
     x = _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, dev)
     Hk, d = Kpages.shape[1], Kpages.shape[3]
@@ -613,6 +625,11 @@ def moda_page_select(Q, Kbounds, page_table, keep, page_rows, lengths=None, firs
     Kbounds [n_pages,Hk,2,d] promise the largest logits, summed over the heads of the group, for the queries Q [B,Hq,d]; indices into
     the sequence's row of page_table [B,max_pages], ascending, -1 behind the last.  lengths [B] (int32; None: T, None: all rows that the
     table has).  What moda_attn_decode_paged takes as `selected`."""
+    if out is not None:
+        r = (_native_module or _native()).page_select(Q, Kbounds, page_table, keep, page_rows, lengths, first, recent, T, out, workspace)
+        if r is not None:
+            _outputs(r)
+            return out
     B, Hq, d = Q.shape
     dev = Q.device
     if Kbounds.dim() != 4 or page_table.dim() != 2:
@@ -643,6 +660,10 @@ def moda_attn_decode_paged(Q, Kpages, Vpages, page_table, Kdepth=None, Vdepth=No
     the cache's arguments; the token's own row is among them) and its depth slots Kdepth/Vdepth [B,Hk,depth_alloc,d] or None.
     lengths [B] (int32): the rows of each sequence; T bounds them (default: all rows that the table has) and is their number where lengths is
     None.  selected [B,Hk,n] (int32): only the rows of these pages, indices into the sequence's row of page_table, each once, -1: none."""
+    r = (_native_module or _native()).paged(Q, Kpages, Vpages, page_table, Kdepth, Vdepth, lengths, selected, Kscales, Vscales, T,
+                                            depth_count, scale, out, lse, workspace)
+    if r is not None:
+        return _outputs(r)
     B, Hq, d = Q.shape
     dev = Q.device
     x = _pages(Kpages, Vpages, page_table, Kscales, Vscales, B, dev)
