@@ -8,6 +8,7 @@
 // launch_decode_paged), so that sequences of any lengths fill the chip evenly; every workgroup adds up the lengths and finds its slice.
 #include <algorithm>
 
+#include "moda_decode_columns.h"
 #include "moda_pages.h"
 
 namespace moda {
@@ -272,6 +273,137 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
   }
 }
 
+// ---------------------------------------------------------------- rows on the matrix pipe
+// A block of 32 rows in flight: pieces of 1 KB of K and of V, and the scales of 8-bit rows.
+template <int D, bool MX>
+struct PageBlock {
+  static constexpr int kInst = 32 * (MX ? D : 2 * D) / 1024;
+  u32x4 k[kInst], v[kInst];
+  unsigned ks[MX ? kInst : 1], vs[MX ? kInst : 1];
+  int left[2];  // rows of the first and the other 16 that count
+};
+
+// Every wave by itself: rows [first, first + n) of the list (first, and n unless the sequence ends, multiples of 32), 32 at a time through its two
+// LDS tiles at `lds`, kPF blocks in flight in registers.  8-bit rows become bf16 on the way to LDS, exactly: 32 conversions per lane and block
+// (d = 128) beside 16 matrix instructions.
+template <int D, bool MX, int kPF>
+__device__ __forceinline__ void read_pages(Columns<D>& c, const PagedParams& p, PageList& list, int g, int first, int n, unsigned lds, float c2) {
+  using Tl = Tile<D>;
+  using Block = PageBlock<D, MX>;
+  constexpr int CB = MX ? D : 2 * D, SB = D / kBlock, kInst = Block::kInst, kRows = 32 / kInst, kHalf = 32 * Tl::kRowBytes;
+  constexpr int LPR = 64 / kRows;  // lanes of a row
+  const int lane = threadIdx.x & 63, jr = lane / LPR, pc = lane % LPR;
+  FragAddr<D> fa;
+  fa.init(lane);
+  // bf16: the chunk that a lane fetches is the one whose place in the tile it fills; 8 bits: its two chunks go to their places
+  const int g_off = MX ? jr * CB + pc * 16 : jr * CB + ((pc ^ Tl::swz(jr)) << 4);
+  const int s_off = jr * SB + pc / 2;
+  const unsigned to = MX ? lds + jr * Tl::kRowBytes + (((2 * pc) ^ Tl::swz(jr)) << 4) : lds + lane * 16;
+  auto piece_xor = [](int q) { return D == 128 ? (MX ? (q & 1) * 32 : (q & 3) << 4) : (MX ? 0 : (q & 1) * 32); };
+  const int n_blocks = (n + 31) / 32;
+  auto issue = [&](int blk, Block& r) {
+    const int row = first + blk * 32;
+    if (blk < n_blocks && ((row + 31) >> p.shift) - list.base >= 64) list.load(p, row >> p.shift, lane);  // (uniform)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = row + h * 16, i = min((at >> p.shift) - list.base, 63), slot = at & ((1 << p.shift) - 1);
+      const int id = __builtin_amdgcn_readlane(list.id, i), count = blk < n_blocks ? __builtin_amdgcn_readlane(list.count, i) : 0;
+      const size_t row0 = ((size_t)id * p.Hk + g) << p.shift;
+      const __amdgpu_buffer_rsrc_t kb = rows_buffer(p.K + row0 * CB, count * CB), vb = rows_buffer(p.V + row0 * CB, count * CB);
+      r.left[h] = count - slot;
+#pragma unroll
+      for (int q = h * kInst / 2; q < (h + 1) * kInst / 2; ++q) {
+        const int at_row = slot + q * kRows - h * 16;
+        const int v_off = MX ? g_off : xor_here(g_off, piece_xor(q));
+        r.k[q] = __builtin_amdgcn_raw_buffer_load_b128(kb, v_off, at_row * CB, 2);
+        r.v[q] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off, at_row * CB, 2);
+      }
+      if (MX) {
+        const __amdgpu_buffer_rsrc_t ksb = rows_buffer(p.Ks + row0 * SB, count * SB), vsb = rows_buffer(p.Vs + row0 * SB, count * SB);
+#pragma unroll
+        for (int q = h * kInst / 2; q < (h + 1) * kInst / 2; ++q) {
+          const int at_row = slot + q * kRows - h * 16;
+          r.ks[q] = __builtin_amdgcn_raw_buffer_load_b8(ksb, s_off, at_row * SB, 0);
+          r.vs[q] = __builtin_amdgcn_raw_buffer_load_b8(vsb, s_off, at_row * SB, 0);
+        }
+      }
+    }
+  };
+  auto store = [&](unsigned at, const u32x4& x) { *(u32x4 __attribute__((address_space(3)))*)(size_t)at = x; };
+  auto stage = [&](const u32x4 (&x)[kInst], const unsigned (&s)[MX ? kInst : 1], int tile) {
+#pragma unroll
+    for (int q = 0; q < kInst; ++q) {
+      if (MX) {
+        const float sc = scale_of(s[q]);
+        const unsigned at = (unsigned)xor_here((int)(to + tile), piece_xor(q)) + q * kRows * Tl::kRowBytes;
+        store(at, (u32x4){codes_bf16<false>(x[q][0], sc), codes_bf16<true>(x[q][0], sc), codes_bf16<false>(x[q][1], sc), codes_bf16<true>(x[q][1], sc)});
+        store(at ^ 16, (u32x4){codes_bf16<false>(x[q][2], sc), codes_bf16<true>(x[q][2], sc), codes_bf16<false>(x[q][3], sc), codes_bf16<true>(x[q][3], sc)});
+      } else {
+        store(to + tile + q * 1024, x[q]);
+      }
+    }
+  };
+  Block buf[kPF];
+#pragma unroll
+  for (int i = 0; i < kPF; ++i) issue(i, buf[i]);
+  for (int blk0 = 0; blk0 < n_blocks; blk0 += kPF) {
+#pragma unroll
+    for (int i = 0; i < kPF; ++i) {
+      const int blk = blk0 + i, lower = buf[i].left[0], upper = buf[i].left[1];
+      // (a wave's LDS operations execute in order: these writes follow the reads of the block before)
+      stage(buf[i].k, buf[i].ks, 0);
+      stage(buf[i].v, buf[i].vs, kHalf);
+      issue(blk + kPF, buf[i]);
+      if (max(lower, upper) > 0)  // (uniform)
+        c.template fold<1, true>(lds, lds + kHalf, fa, lane, lower, c2, nullptr, 0, 0, upper);
+    }
+  }
+}
+
+constexpr int kMatrixHeads = 32;
+template <int D, bool MX>
+__global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(PagedParams p) {
+  constexpr int RB = D * 2, kPF = D == 128 && !MX ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kShWaves * 2 * 32 * RB];
+  __shared__ float stat[kShWaves][32][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hi = lane >> 5;
+  const unsigned lds = (unsigned)(size_t)(lds_ptr)smem + wave * 2 * 32 * RB;
+  const float c2 = p.scale_log2;
+  const int unit = blockIdx.x % p.units, s = blockIdx.x / p.units;
+  const Slice x = find_slice(p, s, lane);
+  if (x.b < 0) return;  // (uniform)
+  const int b = x.b, G = p.Hq / p.Hk, g = unit % p.Hk, gc = unit / p.Hk;
+  const int nh = min(kMatrixHeads, G - gc * kMatrixHeads);
+  const size_t bh = (size_t)b * p.Hq + g * G + gc * kMatrixHeads;
+  if (unit == 0 && s == x.first && tid == 0) {
+    p.ws_deal[2 * b] = x.first;
+    p.ws_deal[2 * b + 1] = x.n;
+  }
+  Columns<D> c;
+  c.init((const char*)p.Q + (bh + min(l32, nh - 1)) * RB, hi);
+  // a wave's part of n rows: a quarter, in whole blocks of 32
+  auto part = [&](int n, int& first) {
+    const int q = ((n + kShWaves - 1) / kShWaves + 31) / 32 * 32;
+    first = min(wave * q, n);
+    return min(q, n - first);
+  };
+  int first;
+  const int n = part(max(min(x.rows - x.begin, x.per), 0), first);
+  if (n > 0) {  // (uniform)
+    PageList list;
+    list.init(p, b, g);
+    list.load(p, (x.begin + first) >> p.shift, lane);
+    read_pages<D, MX, kPF>(c, p, list, g, x.begin + first, n, lds, c2);
+  }
+  if (s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice
+    const int n_slots = part(p.depth_count, first);
+    const size_t at = ((size_t)b * p.Hk + g) * p.depth_alloc * RB + (size_t)first * RB;
+    read_by_wave<D, 1>(c, Rows{p.Kd + at, p.Vd + at, n_slots, nullptr, nullptr, 0}, lds, c2);
+  }
+  const size_t to = (size_t)s * p.Hq + g * G + gc * kMatrixHeads;
+  fold_waves<D, 1>(c, smem, stat, c2, nh, p.ws_o + to * D, p.ws_ml + to * 2);
+}
+
 // ---------------------------------------------------------------- outputs
 // `by` slices of a head at a time, D / 4 threads each (four channels a thread), 1024 / D such teams in a workgroup.
 template <int D>
@@ -345,10 +477,11 @@ __global__ __launch_bounds__(256) void moda_paged_finish_kernel(PagedParams p, i
 // ---------------------------------------------------------------- host side
 static void plan(PagedParams& p, int d, bool mx) {
   const int G = p.Hq / p.Hk;
-  p.heads_per = G <= 2 ? G : 4;
+  p.heads_per = G <= 2 ? G : kMatrixHeads;
   p.units = p.Hk * ((G + p.heads_per - 1) / p.heads_per);
-  p.least = kPgWaves * 4 * 64 * (mx ? 16 : 8) / d;  // what the waves take at a time
-  p.good = std::max(256, p.least);
+  // `least`: what the waves take at a time
+  p.least = G <= 2 ? kPgWaves * 4 * 64 * (mx ? 16 : 8) / d : kShWaves * 32;
+  p.good = G <= 2 ? std::max(256, p.least) : 512;
   // Slices of one size, `least` or more, and one more of every sequence: find_slice's sizes make no more.
   p.n_slices = p.B + kPgMany / p.units;
 }
@@ -367,7 +500,7 @@ static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
   while (by < teams && (long long)by * 4 * p.B < p.n_slices) by *= 2;
   const long long finish_blocks = (heads + teams / by - 1) / (teams / by);
   if (!grid_ok(blocks, kPgWaves * 64) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
-  auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX> : moda_paged_slices_kernel<D, 4, MX>;
+  auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX> : moda_paged_matrix_kernel<D, MX>;
   const hipError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kPgWaves * 64), stream, p);
   if (e != hipSuccess) return e;
   return launch_kernel(moda_paged_finish_kernel<D>, dim3((unsigned)finish_blocks), dim3(256), stream, p, by);
