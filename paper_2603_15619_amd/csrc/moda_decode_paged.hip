@@ -32,7 +32,7 @@ struct Slice {
 __device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) x += __shfl_xor(x, k);
-  return x;
+  return __builtin_amdgcn_readfirstlane(x);  // (so that what is made of it stays out of the vector registers)
 }
 // Slice s of all slices; a wave's lanes look at a sequence each.
 __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lane) {
@@ -42,10 +42,13 @@ __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lan
     rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
     total += ((long long)wave_sum(rows >> 16) << 16) + wave_sum(rows & 0xffff);
   }
-  auto whole = [&](long long n) { return (n + p.least - 1) / p.least * p.least; };
-  const long long few = whole((total * p.units + kPgFew - 1) / kPgFew), many = whole((total * p.units + kPgMany - 1) / kPgMany);
+  // rows of a slice with so many workgroups, in whole steps of 1 << least_shift
+  auto share = [&](int workgroups) {
+    const long long n = total * p.units + workgroups - 1, step = 1ll << p.least_shift;
+    return ((n / workgroups + step - 1) >> p.least_shift) << p.least_shift;
+  };
   Slice r;
-  r.per = (int)max(min(few, max(many, (long long)p.good)), (long long)p.least);
+  r.per = (int)max(min(share(kPgFew), max(share(kPgMany), (long long)p.good)), 1ll << p.least_shift);
   r.b = -1;
   int before = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {  // (uniform)
@@ -479,9 +482,9 @@ static void plan(PagedParams& p, int d, bool mx) {
   const int G = p.Hq / p.Hk;
   p.heads_per = G <= 2 ? G : kMatrixHeads;
   p.units = p.Hk * ((G + p.heads_per - 1) / p.heads_per);
-  // `least`: what the waves take at a time
-  p.least = G <= 2 ? kPgWaves * 4 * 64 * (mx ? 16 : 8) / d : kShWaves * 32;
-  p.good = G <= 2 ? std::max(256, p.least) : 512;
+  const int least = G <= 2 ? kPgWaves * 4 * 64 * (mx ? 16 : 8) / d : kShWaves * 32;  // what the waves take at a time: 64 to 256
+  p.least_shift = __builtin_ctz(least);
+  p.good = G <= 2 ? std::max(256, least) : 512;
   // Slices of one size, `least` or more, and one more of every sequence: find_slice's sizes make no more.
   p.n_slices = p.B + kPgMany / p.units;
 }

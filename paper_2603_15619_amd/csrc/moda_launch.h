@@ -193,7 +193,7 @@ struct PagedParams {
   int n_selected;
   int depth_alloc, depth_count;
   int units, heads_per;  // workgroups of a slice; query heads of one
-  int least, good;       // rows that slices are multiples of; rows of one once the chip is full
+  int least_shift, good;  // 1 << least_shift: rows that slices are multiples of; `good`: rows of one once the chip is full
   int n_slices;          // most slices of all sequences together
   float scale, scale_log2;
 };
