@@ -76,22 +76,10 @@ struct Scorer {
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) x[u] = *(const u32x4*)(bounds + (size_t)max(__shfl(id, u * PPI + lane / LPP), 0) * page_bytes);
   }
-  __device__ __forceinline__ void query(const SelectParams& p, int b, int g) {
-    const int G = p.Hq / p.Hk;
-    const bool high = lane % LPP >= LPP / 2;
+  // The lane's queries from those of the workgroup, [lo, hi][d].
+  __device__ __forceinline__ void query(const double* sums) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = 0.0;
-    const char* at = (const char*)p.Q + ((size_t)b * p.Hq + g * G) * RB + lane % (LPP / 2) * 16;
-#pragma unroll 2
-    for (int h = 0; h < G; ++h) {
-      const u32x4 y = *(const u32x4*)(at + (size_t)h * RB);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float f = i % 2 ? bf16_hi(y[i / 2]) : bf16_lo(y[i / 2]);
-        // (a NaN query counts on both sides)
-        q[i] += f != f || (high ? f > 0.f : f < 0.f) ? (double)f : 0.0;
-      }
-    }
+    for (int i = 0; i < 8; ++i) q[i] = sums[lane % LPP * 8 + i];
   }
   // The page of the batch whose key the lane holds (d = 128: four lanes hold it, d = 64: two, of which one stores it).
   __device__ __forceinline__ int page() const {
@@ -124,175 +112,201 @@ struct Scorer {
   }
 };
 
+// The sums of a group's queries that bounds are multiplied by: down_c, then up_c.  A thread has one of them.
+template <int D, int THREADS>
+__device__ __forceinline__ void query_sums(const SelectParams& p, int b, int g, double* sums) {
+  const int G = p.Hq / p.Hk, t = threadIdx.x;
+  static_assert(THREADS >= 2 * D, "a thread per sum");
+  if (t >= 2 * D) return;
+  const bool high = t >= D;
+  const unsigned short* at = (const unsigned short*)p.Q + ((size_t)b * p.Hq + g * G) * D + t % D;
+  double q = 0.0;
+  for (int h0 = 0; h0 < G; h0 += 8) {
+    unsigned short y[8];
+#pragma unroll
+    for (int h = 0; h < 8; ++h) y[h] = at[(size_t)min(h0 + h, G - 1) * D];
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+      if (h0 + h >= G) break;  // (uniform)
+      const float f = bf16_lo(y[h]);
+      // (a NaN query counts on both sides)
+      q += f != f || (high ? f > 0.f : f < 0.f) ? (double)f : 0.0;
+    }
+  }
+  sums[t] = q;
+}
+
 // ---------------------------------------------------------------- the choice
-// Of n keys (0: no page) the pages of the largest, p.keep of them, to out in ascending order, -1 behind them.  key(i): page i's.
-constexpr int kParts = 1024;
-template <int NT>
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kParts = kThreads, kPer = 4, kChunk = kPer * kThreads;
 struct Choice {
   int hist[kParts];
-  unsigned least, most;  // upper halves of the keys that compete
+  unsigned least, most;  // upper halves of the keys that compete, the least one's bits turned round
   int stay, compete;
   int part, above, in;
-  int count[NT / 64][2];
+  int count[kPer * kWaves];
 };
-template <int NT, class Key>
-__device__ __forceinline__ void choose(Choice<NT>& c, Key&& key, int n, int keep, int* out) {
-  constexpr int NW = NT / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  auto competes = [](u64 k) { return k != 0 && k != kStays; };
-  // Pages with keys above `hi` are kept, and `need` of those in [lo, hi]: the lowest, or (all) every one.
-  u64 lo = 1, hi = kNaNKey;
-  int need = keep;
-  bool all = n <= keep;
-  if (!all) {  // (uniform)
-    if (tid == 0) {
-      c.least = ~0u;
-      c.most = 0;
-      c.stay = c.compete = 0;
+__device__ __forceinline__ bool competes(u64 k) { return k != 0 && k != kStays; }
+
+// Before the keys are formed: an empty histogram, nothing seen.
+__device__ __forceinline__ void choice_start(Choice& c) {
+  for (int i = threadIdx.x; i < kParts; i += kThreads) c.hist[i] = 0;
+  if (threadIdx.x == 0) {
+    c.least = c.most = 0;
+    c.stay = c.compete = 0;
+  }
+}
+// What a thread has seen of the keys; flush: the workgroup gets to know it.
+struct Seen {
+  unsigned least = 0, most = 0;
+  int stay = 0, compete = 0;
+  __device__ __forceinline__ void add(u64 k) {
+    if (competes(k)) {
+      least = max(least, ~(unsigned)(k >> 32));
+      most = max(most, (unsigned)(k >> 32));
+      ++compete;
     }
-    __syncthreads();
-    unsigned least = ~0u, most = 0;
-    int stay = 0, compete = 0;
-    for (int i = tid; i < n; i += NT) {
-      const u64 k = key(i);
-      if (competes(k)) {
-        least = min(least, (unsigned)(k >> 32));
-        most = max(most, (unsigned)(k >> 32));
-        ++compete;
-      }
-      stay += k == kStays;
+    stay += k == kStays;
+  }
+  __device__ __forceinline__ void flush(Choice& c) const {
+    const unsigned a = wave_max(least), z = wave_max(most);
+    const int s = wave_scan(stay), n = wave_scan(compete);
+    if ((threadIdx.x & 63) == 63) {
+      atomicMax(&c.least, a);
+      atomicMax(&c.most, z);
+      atomicAdd(&c.stay, s);
+      atomicAdd(&c.compete, n);
     }
+  }
+};
+
+// Of n keys (0: no page), all seen, the pages of the largest, `keep` of them, to out in ascending order, -1 behind them.  keys: in LDS (LDS: at
+// most kChunk of them, which then stay in registers) or in memory.  A pass takes kChunk keys at a time, kPer a thread.
+template <bool LDS>
+__device__ __forceinline__ void choose(Choice& c, const u64* keys, int n, int keep, int* out) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  u64 held[kPer];
+  auto fetch = [&](int i0) {
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-      least = min(least, (unsigned)__shfl_xor((int)least, x));
-      most = max(most, (unsigned)__shfl_xor((int)most, x));
-      stay += __shfl_xor(stay, x);
-      compete += __shfl_xor(compete, x);
-    }
-    if (lane == 0) {
-      atomicMin(&c.least, least);
-      atomicMax(&c.most, most);
-      atomicAdd(&c.stay, stay);
-      atomicAdd(&c.compete, compete);
-    }
-    __syncthreads();
-    lo = (u64)c.least << 32;
-    hi = (u64)c.most << 32 | 0xffffffffu;
-    need = keep - c.stay;
-    all = c.compete <= need;
-    if (need <= 0) {  // (the pages that stay fill the list)
-      all = false;
-      lo = hi = kStays;
-      need = keep;
-    }
+    for (int j = 0; j < kPer; ++j) held[j] = i0 + j * kThreads + tid < n ? keys[i0 + j * kThreads + tid] : 0;
+  };
+  if (LDS) fetch(0);
+  // Pages with keys above `hi` are kept, and `need` of those in [lo, hi]: the lowest, or (all) every one.
+  u64 lo = (u64)~c.least << 32, hi = (u64)c.most << 32 | 0xffffffffu;
+  int need = keep - c.stay;
+  bool all = c.compete <= need;
+  if (need <= 0) {  // the pages that stay fill the list
+    all = false;
+    lo = hi = kStays;
+    need = keep;
   }
   while (!all && lo < hi) {  // (uniform)
     const int shift = max(54 - __builtin_clzll(hi - lo), 0);  // so that (hi - lo) >> shift is below 1024
-    for (int i = tid; i < kParts; i += NT) c.hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += NT) {
-      const u64 k = key(i);
-      if (competes(k) && k >= lo && k <= hi) atomicAdd(&c.hist[(int)((k - lo) >> shift)], 1);
+    for (int i0 = 0; i0 < n; i0 += kChunk) {
+      if (!LDS) fetch(i0);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (competes(held[j]) && held[j] >= lo && held[j] <= hi) atomicAdd(&c.hist[(int)((held[j] - lo) >> shift)], 1);
     }
     __syncthreads();
-    if (wave == 0) {  // 16 parts a lane, from the largest down
-      constexpr int kPer = kParts / 64;
-      int h[kPer], sum = 0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) sum += h[i] = c.hist[kParts - 1 - lane * kPer - i];
-      int above = sum;
-#pragma unroll
-      for (int x = 1; x < 64; x *= 2) {
-        const int y = __shfl_up(above, x);
-        if (lane >= x) above += y;
-      }
-      above -= sum;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (above < need && above + h[i] >= need) {
-          c.part = kParts - 1 - lane * kPer - i;
-          c.above = above;
-          c.in = h[i];
-        }
-        above += h[i];
-      }
+    // a part a thread, from the largest down; the parts are empty again behind
+    const int h = c.hist[kParts - 1 - tid], to = wave_scan(h);
+    c.hist[kParts - 1 - tid] = 0;
+    if (lane == 63) c.count[wave] = to;
+    __syncthreads();
+    const int of_wave = c.count[lane % kWaves], up_to = row_scan(of_wave);
+    const int above = __builtin_amdgcn_readlane(up_to - of_wave, wave) + to - h;
+    if (above < need && above + h >= need) {
+      c.part = kParts - 1 - tid;
+      c.above = above;
+      c.in = h;
     }
     __syncthreads();
     need -= c.above;
     all = c.in == need;
     lo += (u64)c.part << shift;
     if (hi - lo >= 1ull << shift) hi = lo + ((1ull << shift) - 1);
-    __syncthreads();
   }
-  int before = 0, equal_before = 0;
+  // Counted off: (kept for sure, candidates) of 64 keys each as one number, two times 16 bits; a chunk has 64 of them, a lane's each.
+  int before = 0, in_before = 0;
   const int most = all ? 0x7fffffff : need;
-  for (int i0 = 0; i0 < n; i0 += NT) {  // (uniform)
-    const u64 k = i0 + tid < n ? key(i0 + tid) : 0;
-    const bool more = k > hi, in = k >= lo && !more;
-    const u64 mask_e = __builtin_amdgcn_ballot_w64(in), mask_m = __builtin_amdgcn_ballot_w64(more);
-    if (lane == 0) {
-      c.count[wave][0] = __builtin_popcountll(mask_m);
-      c.count[wave][1] = __builtin_popcountll(mask_e);
+  for (int i0 = 0; i0 < n; i0 += kChunk) {  // (uniform)
+    if (!LDS) {
+      fetch(i0);
+      __syncthreads();  // (the numbers of the chunk before have been read)
+    }
+    u64 more[kPer], in[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      more[j] = __builtin_amdgcn_ballot_w64(held[j] > hi);
+      in[j] = __builtin_amdgcn_ballot_w64(held[j] >= lo && held[j] <= hi);
+      if (lane == 0) c.count[j * kWaves + wave] = __builtin_popcountll(more[j]) << 16 | __builtin_popcountll(in[j]);
     }
     __syncthreads();
-    int m = before, e = equal_before;
-    for (int w = 0; w < NW; ++w) {
-      const int cm = c.count[w][0], ce = c.count[w][1];
-      if (w < wave) {
-        m += cm;
-        e += ce;
-      }
-      before += cm;
-      equal_before += ce;
+    const int own = c.count[lane], to = wave_scan(own);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int at = __builtin_amdgcn_readlane(to - own, j * kWaves + wave);
+      const u64 below = (1ull << lane) - 1;
+      const int m = before + (at >> 16) + __builtin_popcountll(more[j] & below), e = in_before + (at & 0xffff) + __builtin_popcountll(in[j] & below);
+      const bool is_in = in[j] >> lane & 1;
+      if ((more[j] >> lane & 1) || (is_in && e < most)) out[m + min(e, most)] = i0 + j * kThreads + tid;
     }
-    const u64 below = (1ull << lane) - 1;
-    m += __builtin_popcountll(mask_m & below);
-    e += __builtin_popcountll(mask_e & below);
-    if (more || (in && e < most)) out[m + min(e, most)] = i0 + tid;
-    __syncthreads();
+    const int total = __builtin_amdgcn_readlane(to, 63);
+    before += total >> 16;
+    in_before += total & 0xffff;
   }
-  const int kept = before + min(equal_before, most);
-  for (int i = kept + tid; i < keep; i += NT) out[i] = -1;
+  const int kept = before + min(in_before, most);
+  for (int i = kept + tid; i < keep; i += kThreads) out[i] = -1;
 }
 
 // ---------------------------------------------------------------- kernels
-constexpr int kOnePages = 4096;  // of one (sequence, key/value head) in one kernel
 template <int D>
-__global__ __launch_bounds__(1024) void moda_page_select_kernel(SelectParams p) {
-  __shared__ u64 keys[kOnePages];
-  __shared__ Choice<1024> c;
+__global__ __launch_bounds__(kThreads) void moda_page_select_kernel(SelectParams p) {
+  __shared__ u64 keys[kChunk];
+  __shared__ __attribute__((aligned(16))) double sums[2 * D];
+  __shared__ Choice c;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.x / p.Hk, g = blockIdx.x - b * p.Hk, n = pages_filled(p, b);
+  choice_start(c);
   Scorer<D> s;
   s.init(p, b, g, n);
-  int first = (threadIdx.x >> 6) * s.kPages;
-  if (first < n && n > p.keep) {  // (uniform over a wave)
-    s.load(p, first);
-    s.query(p, b, g);
+  int first = wave * s.kPages;
+  Seen seen;
+  const bool choice = n > p.keep;  // (uniform; else all pages that there are)
+  if (choice && first < n) s.load(p, first);
+  if (choice) query_sums<D, kThreads>(p, b, g, sums);
+  __syncthreads();
+  if (!choice) {
+    for (int i = threadIdx.x; i < n; i += kThreads) seen.add(keys[i] = page_at(s.table, i, p.n_pages) < 0 ? 0ull : kStays);
+  } else if (first < n) {  // (uniform over a wave)
+    s.query(sums);
     while (true) {
       const u64 k = s.key(p, first);
-      if (s.stores() && first + s.page() < n) keys[first + s.page()] = k;
-      first += 16 * s.kPages;
+      if (s.stores() && first + s.page() < n) seen.add(keys[first + s.page()] = k);
+      first += kWaves * s.kPages;
       if (first >= n) break;
       s.load(p, first);
     }
-  } else if (n <= p.keep) {  // all pages there are
-    for (int i = threadIdx.x; i < n; i += 1024) keys[i] = page_at(s.table, i, p.n_pages) < 0 ? 0ull : kStays;
   }
+  seen.flush(c);
   __syncthreads();
-  choose<1024>(c, [&](int i) { return keys[i]; }, n, p.keep, p.pages + (size_t)blockIdx.x * p.keep);
+  choose<true>(c, keys, n, p.keep, p.pages + (size_t)blockIdx.x * p.keep);
 }
 
 template <int D>
 __global__ __launch_bounds__(256) void moda_page_score_kernel(SelectParams p, int batches, int chunks) {
+  __shared__ __attribute__((aligned(16))) double sums[2 * D];
   const int bg = blockIdx.x / chunks, b = bg / p.Hk, g = bg - b * p.Hk, n = pages_filled(p, b);
   Scorer<D> s;
   int first = ((blockIdx.x - bg * chunks) * 4 + (threadIdx.x >> 6)) * batches * s.kPages;
   const int end = min(n, first + batches * s.kPages);
-  if (first >= end) return;
   s.init(p, b, g, n);
   u64* keys = p.keys + (size_t)bg * p.cols;
-  s.load(p, first);
-  s.query(p, b, g);
+  if (first < end) s.load(p, first);
+  query_sums<D, 256>(p, b, g, sums);
+  __syncthreads();
+  if (first >= end) return;
+  s.query(sums);
   while (true) {
     const u64 k = s.key(p, first);
     if (s.stores() && first + s.page() < n) keys[first + s.page()] = k;
@@ -301,15 +315,22 @@ __global__ __launch_bounds__(256) void moda_page_score_kernel(SelectParams p, in
     s.load(p, first);
   }
 }
-__global__ __launch_bounds__(1024) void moda_page_choose_kernel(SelectParams p) {
-  __shared__ Choice<1024> c;
+__global__ __launch_bounds__(kThreads) void moda_page_choose_kernel(SelectParams p) {
+  __shared__ Choice c;
   const u64* keys = p.keys + (size_t)blockIdx.x * p.cols;
-  choose<1024>(c, [&](int i) { return keys[i]; }, pages_filled(p, blockIdx.x / p.Hk), p.keep, p.pages + (size_t)blockIdx.x * p.keep);
+  const int n = pages_filled(p, blockIdx.x / p.Hk);
+  choice_start(c);
+  __syncthreads();
+  Seen seen;
+  for (int i = threadIdx.x; i < n; i += kThreads) seen.add(keys[i]);
+  seen.flush(c);
+  __syncthreads();
+  choose<false>(c, keys, n, p.keep, p.pages + (size_t)blockIdx.x * p.keep);
 }
 
 static int columns(const SelectParams& p) { return (int)(((long long)p.T + (1 << p.shift) - 1) >> p.shift); }
 
-static bool in_one(const SelectParams& p) { return columns(p) <= kOnePages; }
+static bool in_one(const SelectParams& p) { return columns(p) <= kChunk; }
 
 size_t select_workspace_bytes(const SelectParams& p) { return (size_t)p.B * p.Hk * columns(p) * sizeof(u64); }
 
@@ -317,9 +338,9 @@ hipError_t launch_select(SelectParams p, int d, void* workspace, hipStream_t str
   p.cols = columns(p);
   p.keys = (u64*)workspace;
   const long long groups = (long long)p.B * p.Hk;
-  if (!grid_ok(groups, 1024)) return kGridTooLarge;
+  if (!grid_ok(groups, kThreads)) return kGridTooLarge;
   if (in_one(p))
-    return launch_kernel(d == 128 ? moda_page_select_kernel<128> : moda_page_select_kernel<64>, dim3((unsigned)groups), dim3(1024), stream, p);
+    return launch_kernel(d == 128 ? moda_page_select_kernel<128> : moda_page_select_kernel<64>, dim3((unsigned)groups), dim3(kThreads), stream, p);
   // a wave takes several batches of pages where there are more than 16 waves a compute unit
   const int per_batch = 8 * 256 / d;
   const long long all = groups * ((p.cols + per_batch - 1) / per_batch);
@@ -329,7 +350,7 @@ hipError_t launch_select(SelectParams p, int d, void* workspace, hipStream_t str
   const hipError_t e = launch_kernel(d == 128 ? moda_page_score_kernel<128> : moda_page_score_kernel<64>, dim3((unsigned)(groups * chunks)),
                                      dim3(256), stream, p, batches, chunks);
   if (e != hipSuccess) return e;
-  return launch_kernel(moda_page_choose_kernel, dim3((unsigned)groups), dim3(1024), stream, p);
+  return launch_kernel(moda_page_choose_kernel, dim3((unsigned)groups), dim3(kThreads), stream, p);
 }
 
 }  // namespace moda

@@ -37,6 +37,35 @@ __device__ __forceinline__ f32x2 codes_f32(uint32_t codes, float scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, HI);
 }
 
+// Sums over a wave's lanes up to and with the own one, of non-negative numbers (in registers: a shuffle through LDS takes ten times as long).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_zero(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int row_scan(int x) {  // over the lanes of a row of 16
+  x += dpp_or_zero<0x111, 0xf>(x);  // row_shr:1
+  x += dpp_or_zero<0x112, 0xf>(x);
+  x += dpp_or_zero<0x114, 0xf>(x);
+  x += dpp_or_zero<0x118, 0xf>(x);
+  return x;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = row_scan(x);
+  x += dpp_or_zero<0x142, 0xa>(x);  // row_bcast:15 to rows 1 and 3
+  x += dpp_or_zero<0x143, 0xc>(x);  // row_bcast:31 to rows 2 and 3
+  return x;
+}
+
+// The largest of a wave's numbers, in its last lane.
+__device__ __forceinline__ unsigned wave_max(unsigned x) {
+  x = max(x, (unsigned)dpp_or_zero<0x111, 0xf>((int)x));
+  x = max(x, (unsigned)dpp_or_zero<0x112, 0xf>((int)x));
+  x = max(x, (unsigned)dpp_or_zero<0x114, 0xf>((int)x));
+  x = max(x, (unsigned)dpp_or_zero<0x118, 0xf>((int)x));
+  x = max(x, (unsigned)dpp_or_zero<0x142, 0xa>((int)x));
+  return max(x, (unsigned)dpp_or_zero<0x143, 0xc>((int)x));
+}
+
 // The physical page of logical page i of a sequence whose row of the table is `table`; -1: none.
 __device__ __forceinline__ int page_at(const int* table, int i, int n_pages) {
   const int id = table[i];
