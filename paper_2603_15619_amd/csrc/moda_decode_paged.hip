@@ -29,11 +29,7 @@ struct Slice {
   int per;          // rows of a slice
   int first, n;     // the sequence's first slice, and how many it has
 };
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) x += __shfl_xor(x, k);
-  return __builtin_amdgcn_readfirstlane(x);  // (so that what is made of it stays out of the vector registers)
-}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 // Slice s of all slices; a wave's lanes look at a sequence each.
 __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lane) {
   long long total = 0;  // (thousands of rows would do 32 bits, a large batch of long ones not: 16 bits at a time)
@@ -54,13 +50,7 @@ __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lan
   for (int b0 = 0; b0 < p.B; b0 += 64) {  // (uniform)
     if (p.B > 64) rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
     const int n = b0 + lane < p.B ? max((int)(((unsigned)rows + r.per - 1) / (unsigned)r.per), 1) : 0;
-    int to = n;  // of this sequence and those before it
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) {
-      const int x = __shfl_up(to, k);
-      if (lane >= k) to += x;
-    }
-    to += before;
+    const int to = before + wave_scan(n);  // of this sequence and those before it
     const unsigned long long behind = __builtin_amdgcn_ballot_w64(to > s);
     if (behind) {  // (uniform)
       const int i = __builtin_ctzll(behind);
