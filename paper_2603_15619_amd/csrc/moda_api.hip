@@ -671,7 +671,7 @@ static moda::PagedParams paged_dims(const moda_pages* x, const moda_shape* s) {
 
 size_t moda_attn_decode_paged_workspace_bytes(const moda_pages* x, const moda_shape* s) {
   if (check_decode_paged(x, s) != MODA_OK || s->B == 0) return 0;
-  return moda::decode_paged_workspace_bytes(paged_dims(x, s), s->d);
+  return moda::decode_paged_workspace_bytes(paged_dims(x, s), s->d, x->type == MODA_PAGES_MX8);
 }
 
 moda_status moda_attn_decode_paged(const void* Q, const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales,
@@ -690,7 +690,7 @@ moda_status moda_attn_decode_paged(const void* Q, const void* Kpages, const void
     if (!aligned16(q)) return MODA_ERR_ALIGN;
   if (!aligned4(page_table) || !aligned4(lengths) || !aligned4(selected)) return MODA_ERR_ALIGN;
   moda::PagedParams p = paged_dims(x, s);
-  if (!workspace || workspace_bytes < moda::decode_paged_workspace_bytes(p, s->d)) return MODA_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < moda::decode_paged_workspace_bytes(p, s->d, x->type == MODA_PAGES_MX8)) return MODA_ERR_WORKSPACE;
   p.Q = Q; p.K = (const char*)Kpages; p.V = (const char*)Vpages;
   p.Ks = (const unsigned char*)Kscales; p.Vs = (const unsigned char*)Vscales;
   p.table = page_table; p.lengths = lengths;

@@ -14,8 +14,10 @@
 namespace moda {
 
 constexpr int kPgWaves = 4;
-// Workgroups that the cut aims at: as many as there are compute units as long as their slices have `least` rows, twice that with `good`.
-constexpr int kPgFew = 256, kPgMany = 512;
+// Workgroups that the cut aims at, and the least rows that it gives them: one per compute unit (whole steps of the waves), as many as are
+// resident at once, and, where slices are long, several rounds of them: workgroups do not get equal shares of the memory's rate, and
+// in one round the slowest decide.
+constexpr int kPgFew = 256, kPgOnce = 512, kPgOnceRows = 512, kPgMany = 2048;
 
 // ---------------------------------------------------------------- the cut
 // Rows of a sequence: of its cache, or of the places on its lists (whole pages: what a page holds is looked at later).
@@ -26,7 +28,7 @@ __device__ __forceinline__ int paged_rows(const PagedParams& p, int b) {
 struct Slice {
   int b;            // -1: no such slice
   int begin, rows;  // its first row, and all rows of the sequence
-  int per;          // rows of a slice
+  int per;          // rows of its slices
   int first, n;     // the sequence's first slice, and how many it has
 };
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
@@ -43,13 +45,14 @@ __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lan
     const long long n = total * p.units + workgroups - 1, step = 1ll << p.least_shift;
     return ((n / workgroups + step - 1) >> p.least_shift) << p.least_shift;
   };
+  const long long once = max(share(kPgOnce), (long long)kPgOnceRows), many = max(share(kPgMany), (long long)p.good);
+  const unsigned per = (unsigned)max(min(share(kPgFew), min(once, many)), 1ll << p.least_shift);
   Slice r;
-  r.per = (int)max(min(share(kPgFew), max(share(kPgMany), (long long)p.good)), 1ll << p.least_shift);
   r.b = -1;
   int before = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {  // (uniform)
     if (p.B > 64) rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
-    const int n = b0 + lane < p.B ? max((int)(((unsigned)rows + r.per - 1) / (unsigned)r.per), 1) : 0;
+    const int n = b0 + lane < p.B ? max((int)(((unsigned)rows + per - 1) / per), 1) : 0;
     const int to = before + wave_scan(n);  // of this sequence and those before it
     const unsigned long long behind = __builtin_amdgcn_ballot_w64(to > s);
     if (behind) {  // (uniform)
@@ -58,7 +61,9 @@ __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lan
       r.rows = __builtin_amdgcn_readlane(rows, i);
       r.n = __builtin_amdgcn_readlane(n, i);
       r.first = __builtin_amdgcn_readlane(to, i) - r.n;
-      r.begin = (s - r.first) * r.per;
+      // (as many slices, of the same size)
+      r.per = ((((unsigned)r.rows + r.n - 1) / (unsigned)r.n + (1u << p.least_shift) - 1) >> p.least_shift) << p.least_shift;
+      r.begin = min((s - r.first) * r.per, r.rows);
       return r;
     }
     before = __builtin_amdgcn_readlane(to, 63);
@@ -468,26 +473,34 @@ __global__ __launch_bounds__(256) void moda_paged_finish_kernel(PagedParams p, i
 }
 
 // ---------------------------------------------------------------- host side
+// Slices of all sequences together that find_slice makes of at most so many rows: one of every sequence and as many as have its size.
+static int most_slices(const PagedParams& p, long long rows) {
+  auto of = [&](long long workgroups, long long least) { return std::min(workgroups / p.units, rows / least); };
+  return p.B + (int)std::max(of(kPgFew, 1ll << p.least_shift), std::max(of(kPgOnce, kPgOnceRows), of(kPgMany, p.good)));
+}
+
 static void plan(PagedParams& p, int d, bool mx) {
   const int G = p.Hq / p.Hk;
   p.heads_per = G <= 2 ? G : kMatrixHeads;
   p.units = p.Hk * ((G + p.heads_per - 1) / p.heads_per);
   const int least = G <= 2 ? kPgWaves * 4 * 64 * (mx ? 16 : 8) / d : kShWaves * 32;  // what the waves take at a time: 64 to 256
   p.least_shift = __builtin_ctz(least);
-  p.good = G <= 2 ? std::max(256, least) : 512;
-  // Slices of one size, `least` or more, and one more of every sequence: find_slice's sizes make no more.
-  p.n_slices = p.B + kPgMany / p.units;
+  // Rows of a slice in several rounds (us, rows / heads per group; 512 workgroups / 2048 of 512 rows or more / 2048 of 2048 or more):
+  //   vector ALUs    8 x 65536 rows, 16 heads, d = 128: 577 / 525 / 525;  4 x 16000, 16 heads 74.8 / 69.4 / 74.9;  32 x 4000 8-bit, 8 heads 42.0 / 40.2 / 42.3
+  //   matrix pipe    32 x 16000 8-bit, 64 heads on 8, d = 128: 120.5 / 121.2 / 112.8;  64 x 16000 bf16 538 / 505 / 504;  4 x 30000, 64 on 4 39.2 / 45.6 / 40.5
+  p.good = G <= 2 ? 512 : 2048;
+  p.n_slices = most_slices(p, 1ll << 40);
 }
 
-size_t decode_paged_workspace_bytes(const PagedParams& dims, int d) {
-  // (whichever way the rows are read: one head per workgroup makes the fewest units)
-  const size_t slices = (size_t)dims.B + kPgMany / dims.Hk;
-  return (slices * dims.Hq * (d + 2) + 2 * (size_t)dims.B) * sizeof(float);
+size_t decode_paged_workspace_bytes(const PagedParams& dims, int d, bool mx) {
+  PagedParams p = dims;
+  plan(p, d, mx);
+  return ((size_t)p.n_slices * p.Hq * (d + 2) + 2 * (size_t)p.B) * sizeof(float);
 }
 
 template <int D, bool MX>
 static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
-  const long long blocks = (long long)p.units * p.n_slices, heads = (long long)p.B * p.Hq;
+  const long long rows = p.selected ? (long long)p.n_selected << p.shift : p.T, blocks = (long long)p.units * most_slices(p, p.B * rows), heads = (long long)p.B * p.Hq;
   constexpr int teams = 1024 / D;
   int by = 1;  // teams that share a head's slices, so that each folds about four of them at a time
   while (by < teams && (long long)by * 4 * p.B < p.n_slices) by *= 2;

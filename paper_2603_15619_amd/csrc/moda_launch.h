@@ -193,11 +193,11 @@ struct PagedParams {
   int n_selected;
   int depth_alloc, depth_count;
   int units, heads_per;  // workgroups of a slice; query heads of one
-  int least_shift, good;  // 1 << least_shift: rows that slices are multiples of; `good`: rows of one once the chip is full
-  int n_slices;          // most slices of all sequences together
+  int least_shift, good;  // slices: multiples of 1 << least_shift rows; `good` or more where they take several rounds
+  int n_slices;          // most slices of all sequences together, whatever their lengths
   float scale, scale_log2;
 };
-size_t decode_paged_workspace_bytes(const PagedParams& p, int d);
+size_t decode_paged_workspace_bytes(const PagedParams& p, int d, bool mx);
 hipError_t launch_decode_paged(PagedParams p, int d, bool mx, void* workspace, hipStream_t stream);
 
 // Matrix-pipe calibration kernel (moda_calibrate.hip).
