@@ -71,6 +71,12 @@ __device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lan
   return r;
 }
 
+// The one slice of sequence b.
+__device__ __forceinline__ Slice whole_sequence(const PagedParams& p, int b) {
+  const int rows = paged_rows(p, b);
+  return Slice{b, 0, rows, rows, b, 1};
+}
+
 // ---------------------------------------------------------------- pages
 // 64 pages of a sequence's list from page `base` on, one a lane: its number in the pool, and the rows that the sequence has in it.
 struct PageList {
@@ -188,12 +194,12 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane % LPR, rg = lane / LPR;
   const float c2 = p.scale_log2;
   const int unit = blockIdx.x % p.units, s = blockIdx.x / p.units;
-  const Slice x = find_slice(p, s, lane);
+  const Slice x = p.single ? whole_sequence(p, s) : find_slice(p, s, lane);
   if (x.b < 0) return;  // (uniform)
   const int b = x.b, G = p.Hq / p.Hk, g = unit % p.Hk, gc = unit / p.Hk;
   const int nh = min(GT, G - gc * GT);
   const size_t bh = (size_t)b * p.Hq + g * G + gc * GT;
-  if (unit == 0 && s == x.first && tid == 0) {
+  if (unit == 0 && s == x.first && tid == 0 && !p.single) {
     p.ws_deal[2 * b] = x.first;
     p.ws_deal[2 * b + 1] = x.n;
   }
@@ -266,8 +272,14 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
     const int j = t / D, ch = t % D;
     float o;
     const f32x2 ml = fold_rows<D, GT, kPgWaves>(red, j, ch, c2, o);
-    p.ws_o[to * D + t] = o;
-    if (ch == 0) *(f32x2*)(p.ws_ml + (to + j) * 2) = ml;
+    if (p.single) {  // (uniform)
+      const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
+      ((__bf16*)p.O)[bh * D + t] = (__bf16)(none ? 0.f : o / ml[1]);
+      if (ch == 0) p.LSE[bh + j] = none ? -INFINITY : ml[0] * p.scale + __logf(ml[1]);
+    } else {
+      p.ws_o[to * D + t] = o;
+      if (ch == 0) *(f32x2*)(p.ws_ml + (to + j) * 2) = ml;
+    }
   }
 }
 
@@ -368,12 +380,12 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
   const unsigned lds = (unsigned)(size_t)(lds_ptr)smem + wave * 2 * 32 * RB;
   const float c2 = p.scale_log2;
   const int unit = blockIdx.x % p.units, s = blockIdx.x / p.units;
-  const Slice x = find_slice(p, s, lane);
+  const Slice x = p.single ? whole_sequence(p, s) : find_slice(p, s, lane);
   if (x.b < 0) return;  // (uniform)
   const int b = x.b, G = p.Hq / p.Hk, g = unit % p.Hk, gc = unit / p.Hk;
   const int nh = min(kMatrixHeads, G - gc * kMatrixHeads);
   const size_t bh = (size_t)b * p.Hq + g * G + gc * kMatrixHeads;
-  if (unit == 0 && s == x.first && tid == 0) {
+  if (unit == 0 && s == x.first && tid == 0 && !p.single) {
     p.ws_deal[2 * b] = x.first;
     p.ws_deal[2 * b + 1] = x.n;
   }
@@ -399,7 +411,18 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
     read_by_wave<D, 1>(c, Rows{p.Kd + at, p.Vd + at, n_slots, nullptr, nullptr, 0}, lds, c2);
   }
   const size_t to = (size_t)s * p.Hq + g * G + gc * kMatrixHeads;
-  fold_waves<D, 1>(c, smem, stat, c2, nh, p.ws_o + to * D, p.ws_ml + to * 2);
+  fold_waves<D, 1>(c, smem, stat, c2, nh, [&](int j, int piece, const f32x4& o, const f32x2& ml) {
+    if (p.single) {  // (uniform)
+      const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
+      const float inv = none ? 0.f : 1.f / ml[1];
+      *(u32x2*)((__bf16*)p.O + (bh + j) * D + piece * 4) =
+          none ? (u32x2){0u, 0u} : (u32x2){pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+      if (piece == 0) p.LSE[bh + j] = none ? -INFINITY : ml[0] * p.scale + __logf(ml[1]);
+    } else {
+      *(f32x4*)(p.ws_o + (to + j) * D + piece * 4) = o;
+      if (piece == 0) *(f32x2*)(p.ws_ml + (to + j) * 2) = ml;
+    }
+  });
 }
 
 // ---------------------------------------------------------------- outputs
@@ -473,6 +496,20 @@ __global__ __launch_bounds__(256) void moda_paged_finish_kernel(PagedParams p, i
 }
 
 // ---------------------------------------------------------------- host side
+// Rows that a sequence may have: the lengths themselves are on the device.
+static long long rows_bound(const PagedParams& p) { return p.selected ? (long long)p.n_selected << p.shift : p.T; }
+
+// Sequences of one slice each need no second kernel: where they are short, and longer ones where they fill the chip anyway.  Two kernels / one,
+// us, (batch x key/value heads), rows:
+//   bf16, d = 128   1 head   8, 100 7.8 / 4.6;   64, 400 8.6 / 7.4;   8, 700 8.1 / 9.8;   512, 1000 39.5 / 36.2;   8 heads   64, 100 11.1 / 6.8;   8, 400 10.7 / 10.3;
+//                   8, 700 10.6 / 12.5;   512, 1000 49.6 / 39.2
+//   bf16, d = 64    1 head   8, 700 8.1 / 6.7;   8, 1000 8.1 / 7.9;   4 heads   8, 700 9.9 / 8.8;   8, 1000 10.1 / 10.2
+//   8 bits, d = 128   1 head   8, 400 8.3 / 6.9;   8, 700 8.5 / 8.6;   8 heads   8, 400 11.7 / 10.6;   8, 700 11.7 / 13.2;   d = 64   1 head   8, 1000 8.6 / 6.9;   4 heads   8, 1000 10.3 / 11.0
+static bool in_one(const PagedParams& p, int d, bool mx) {
+  const long long rows = rows_bound(p);
+  return rows * d <= (mx && p.heads_per <= 2 ? 80000 : 53000) || (rows <= 1024 && (long long)p.B * p.units >= 256);
+}
+
 // Slices of all sequences together that find_slice makes of at most so many rows: one of every sequence and as many as have its size.
 static int most_slices(const PagedParams& p, long long rows) {
   auto of = [&](long long workgroups, long long least) { return std::min(workgroups / p.units, rows / least); };
@@ -500,7 +537,7 @@ size_t decode_paged_workspace_bytes(const PagedParams& dims, int d, bool mx) {
 
 template <int D, bool MX>
 static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
-  const long long rows = p.selected ? (long long)p.n_selected << p.shift : p.T, blocks = (long long)p.units * most_slices(p, p.B * rows), heads = (long long)p.B * p.Hq;
+  const long long rows = rows_bound(p), blocks = (long long)p.units * (p.single ? p.B : most_slices(p, p.B * rows)), heads = (long long)p.B * p.Hq;
   constexpr int teams = 1024 / D;
   int by = 1;  // teams that share a head's slices, so that each folds about four of them at a time
   while (by < teams && (long long)by * 4 * p.B < p.n_slices) by *= 2;
@@ -508,12 +545,13 @@ static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
   if (!grid_ok(blocks, kPgWaves * 64) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
   auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX> : moda_paged_matrix_kernel<D, MX>;
   const hipError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kPgWaves * 64), stream, p);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || p.single) return e;
   return launch_kernel(moda_paged_finish_kernel<D>, dim3((unsigned)finish_blocks), dim3(256), stream, p, by);
 }
 
 hipError_t launch_decode_paged(PagedParams p, int d, bool mx, void* workspace, hipStream_t stream) {
   plan(p, d, mx);
+  p.single = in_one(p, d, mx);
   p.ws_o = (float*)workspace;
   p.ws_ml = p.ws_o + (size_t)p.n_slices * p.Hq * d;
   p.ws_deal = (int*)(p.ws_ml + (size_t)p.n_slices * p.Hq * 2);

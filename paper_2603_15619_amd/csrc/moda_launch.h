@@ -193,6 +193,7 @@ struct PagedParams {
   int n_selected;
   int depth_alloc, depth_count;
   int units, heads_per;  // workgroups of a slice; query heads of one
+  int single;             // a sequence has one slice, whose workgroups write O and LSE
   int least_shift, good;  // slices: multiples of 1 << least_shift rows; `good` or more where they take several rounds
   int n_slices;          // most slices of all sequences together, whatever their lengths
   float scale, scale_log2;
