@@ -1,6 +1,8 @@
 // Softmax states of up to 32 queries as the columns of matrix products, for the decoding kernels: S^T = K Q^T, O^T += V^T P^T, rows of K
 // and V from LDS.
 #pragma once
+#include <type_traits>
+
 #include "moda_decode_fold.h"
 #include "moda_tile.h"
 
@@ -131,12 +133,14 @@ struct Columns {
   }
 };
 
-// The states of a workgroup's waves, those with the same columns (wave % CW) folded, of the first n of CW * 32 columns: put(column, piece of four
-// channels, their sums, (reference, normaliser)), or to adjacent states in memory.  LDS: a wave's O^T as 16-byte pieces of four channels, piece c of column q at 32 c + (q ^ c % 32) of
+// The states of a workgroup's waves, those with the same columns (wave % CW) folded, of the first n of CW * 32 columns: to adjacent states in memory, or put(column,
+// piece of four channels, their sums, (reference, normaliser)).  LDS: a wave's O^T as 16-byte pieces of four channels, piece c of column q at 32 c + (q ^ c % 32) of
 // the wave's part, so that both the writes (32 columns of a piece) and the reads (the pieces of a column, which make
 // whole rows in memory) touch every bank alike.
-template <int D, int CW, class Put>
-__device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* smem, float (*stat)[32][2], float c2, int n, Put&& put) {
+struct ToMemory {};
+template <int D, int CW, class Put = ToMemory>
+__device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* smem, float (*stat)[32][2], float c2, int n, float* o_out,
+                                           float* ml_out, Put&& put = {}) {
   constexpr int KW = kShWaves / CW, kPieces = D / 4, kPart = 32 * D * 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hi = lane >> 5;
   const float l_all = pair_sum(c.l);
@@ -172,16 +176,13 @@ __device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* s
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += f * x[j];
     }
-    put(col, piece, o, (f32x2){m, l});
+    if constexpr (std::is_same_v<Put, ToMemory>) {
+      *(f32x4*)(o_out + col * D + piece * 4) = o;
+      if (piece == 0) *(f32x2*)(ml_out + col * 2) = (f32x2){m, l};
+    } else {
+      put(col, piece, o, (f32x2){m, l});
+    }
   }
-}
-template <int D, int CW>
-__device__ __forceinline__ void fold_waves(const Columns<D>& c, unsigned char* smem, float (*stat)[32][2], float c2, int n, float* o_out,
-                                           float* ml_out) {
-  fold_waves<D, CW>(c, smem, stat, c2, n, [&](int col, int piece, const f32x4& o, const f32x2& ml) {
-    *(f32x4*)(o_out + col * D + piece * 4) = o;
-    if (piece == 0) *(f32x2*)(ml_out + col * 2) = ml;
-  });
 }
 
 // Every wave by itself: the rows x, 32 at a time through its two LDS tiles at `lds`; the next block(s) are in flight in

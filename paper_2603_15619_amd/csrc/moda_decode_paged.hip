@@ -411,7 +411,7 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
     read_by_wave<D, 1>(c, Rows{p.Kd + at, p.Vd + at, n_slots, nullptr, nullptr, 0}, lds, c2);
   }
   const size_t to = (size_t)s * p.Hq + g * G + gc * kMatrixHeads;
-  fold_waves<D, 1>(c, smem, stat, c2, nh, [&](int j, int piece, const f32x4& o, const f32x2& ml) {
+  fold_waves<D, 1>(c, smem, stat, c2, nh, nullptr, nullptr, [&](int j, int piece, const f32x4& o, const f32x2& ml) {
     if (p.single) {  // (uniform)
       const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
       const float inv = none ? 0.f : 1.f / ml[1];
