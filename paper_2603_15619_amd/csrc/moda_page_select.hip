@@ -10,9 +10,9 @@
 // Scores: a wave reads the bounds of 16 pages (d = 64: 32) with 8 loads in flight, eight channels per lane, and folds the 8 partial sums of
 // a lane and its neighbours so that every exchange halves what a lane holds: 9 additions in 64 bits (d = 64: 8) for 8 loads.  A score becomes a
 // 64-bit integer of the same order.  The choice: the least key that is kept lies in a range of keys, at first from the least to the
-// largest; a histogram of 1024 parts of the range narrows it until all candidates in it are kept or are equal (then the lowest
+// largest; a histogram of 256 or 1024 parts of the range narrows it until all candidates in it are kept or are equal (then the lowest
 // pages are).  Kept pages are counted off in ascending order.
-// Few pages per (sequence, key/value head): one workgroup of 16 waves does both, keys in LDS; more: two kernels, keys in the workspace.
+// Few pages per (sequence, key/value head), or many such: a workgroup does both, keys in LDS; else two kernels, keys in the workspace.
 #include <algorithm>
 
 #include "moda_pages.h"
@@ -137,9 +137,12 @@ __device__ __forceinline__ void query_sums(const SelectParams& p, int b, int g, 
 }
 
 // ---------------------------------------------------------------- the choice
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kParts = kThreads, kPer = 4, kChunk = kPer * kThreads;
+constexpr int kPer = 4;  // keys of a thread
+// ... by a workgroup of so many threads, each of which has a part of the histogram
+template <int THREADS>
 struct Choice {
-  int hist[kParts];
+  static constexpr int kWaves = THREADS / 64, kChunk = kPer * THREADS;
+  int hist[THREADS];
   unsigned least, most;  // upper halves of the keys that compete, the least one's bits turned round
   int stay, compete;
   int part, above, in;
@@ -148,8 +151,9 @@ struct Choice {
 __device__ __forceinline__ bool competes(u64 k) { return k != 0 && k != kStays; }
 
 // Before the keys are formed: an empty histogram, nothing seen.
-__device__ __forceinline__ void choice_start(Choice& c) {
-  for (int i = threadIdx.x; i < kParts; i += kThreads) c.hist[i] = 0;
+template <int THREADS>
+__device__ __forceinline__ void choice_start(Choice<THREADS>& c) {
+  c.hist[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     c.least = c.most = 0;
     c.stay = c.compete = 0;
@@ -167,7 +171,8 @@ struct Seen {
     }
     stay += k == kStays;
   }
-  __device__ __forceinline__ void flush(Choice& c) const {
+  template <int THREADS>
+  __device__ __forceinline__ void flush(Choice<THREADS>& c) const {
     const unsigned a = wave_max(least), z = wave_max(most);
     const int s = wave_scan(stay), n = wave_scan(compete);
     if ((threadIdx.x & 63) == 63) {
@@ -181,13 +186,14 @@ struct Seen {
 
 // Of n keys (0: no page), all seen, the pages of the largest, `keep` of them, to out in ascending order, -1 behind them.  keys: in LDS (LDS: at
 // most kChunk of them, which then stay in registers) or in memory.  A pass takes kChunk keys at a time, kPer a thread.
-template <bool LDS>
-__device__ __forceinline__ void choose(Choice& c, const u64* keys, int n, int keep, int* out) {
+template <bool LDS, int THREADS>
+__device__ __forceinline__ void choose(Choice<THREADS>& c, const u64* keys, int n, int keep, int* out) {
+  constexpr int kWaves = Choice<THREADS>::kWaves, kChunk = Choice<THREADS>::kChunk;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   u64 held[kPer];
   auto fetch = [&](int i0) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) held[j] = i0 + j * kThreads + tid < n ? keys[i0 + j * kThreads + tid] : 0;
+    for (int j = 0; j < kPer; ++j) held[j] = i0 + j * THREADS + tid < n ? keys[i0 + j * THREADS + tid] : 0;
   };
   if (LDS) fetch(0);
   // Pages with keys above `hi` are kept, and `need` of those in [lo, hi]: the lowest, or (all) every one.
@@ -200,7 +206,7 @@ __device__ __forceinline__ void choose(Choice& c, const u64* keys, int n, int ke
     need = keep;
   }
   while (!all && lo < hi) {  // (uniform)
-    const int shift = max(54 - __builtin_clzll(hi - lo), 0);  // so that (hi - lo) >> shift is below 1024
+    const int shift = max(64 - __builtin_ctz(THREADS) - __builtin_clzll(hi - lo), 0);  // so that (hi - lo) >> shift is below THREADS
     for (int i0 = 0; i0 < n; i0 += kChunk) {
       if (!LDS) fetch(i0);
 #pragma unroll
@@ -209,14 +215,14 @@ __device__ __forceinline__ void choose(Choice& c, const u64* keys, int n, int ke
     }
     __syncthreads();
     // a part a thread, from the largest down; the parts are empty again behind
-    const int h = c.hist[kParts - 1 - tid], to = wave_scan(h);
-    c.hist[kParts - 1 - tid] = 0;
+    const int h = c.hist[THREADS - 1 - tid], to = wave_scan(h);
+    c.hist[THREADS - 1 - tid] = 0;
     if (lane == 63) c.count[wave] = to;
     __syncthreads();
     const int of_wave = c.count[lane % kWaves], up_to = row_scan(of_wave);
     const int above = __builtin_amdgcn_readlane(up_to - of_wave, wave) + to - h;
     if (above < need && above + h >= need) {
-      c.part = kParts - 1 - tid;
+      c.part = THREADS - 1 - tid;
       c.above = above;
       c.in = h;
     }
@@ -226,7 +232,7 @@ __device__ __forceinline__ void choose(Choice& c, const u64* keys, int n, int ke
     lo += (u64)c.part << shift;
     if (hi - lo >= 1ull << shift) hi = lo + ((1ull << shift) - 1);
   }
-  // Counted off: (kept for sure, candidates) of 64 keys each as one number, two times 16 bits; a chunk has 64 of them, a lane's each.
+  // Counted off: (kept for sure, candidates) of 64 keys each as one number, two times 16 bits; a chunk has at most 64 of them, a lane's each.
   int before = 0, in_before = 0;
   const int most = all ? 0x7fffffff : need;
   for (int i0 = 0; i0 < n; i0 += kChunk) {  // (uniform)
@@ -242,29 +248,30 @@ __device__ __forceinline__ void choose(Choice& c, const u64* keys, int n, int ke
       if (lane == 0) c.count[j * kWaves + wave] = __builtin_popcountll(more[j]) << 16 | __builtin_popcountll(in[j]);
     }
     __syncthreads();
-    const int own = c.count[lane], to = wave_scan(own);
+    const int own = lane < kPer * kWaves ? c.count[lane] : 0, to = wave_scan(own);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int at = __builtin_amdgcn_readlane(to - own, j * kWaves + wave);
       const u64 below = (1ull << lane) - 1;
       const int m = before + (at >> 16) + __builtin_popcountll(more[j] & below), e = in_before + (at & 0xffff) + __builtin_popcountll(in[j] & below);
       const bool is_in = in[j] >> lane & 1;
-      if ((more[j] >> lane & 1) || (is_in && e < most)) out[m + min(e, most)] = i0 + j * kThreads + tid;
+      if ((more[j] >> lane & 1) || (is_in && e < most)) out[m + min(e, most)] = i0 + j * THREADS + tid;
     }
     const int total = __builtin_amdgcn_readlane(to, 63);
     before += total >> 16;
     in_before += total & 0xffff;
   }
   const int kept = before + min(in_before, most);
-  for (int i = kept + tid; i < keep; i += kThreads) out[i] = -1;
+  for (int i = kept + tid; i < keep; i += THREADS) out[i] = -1;
 }
 
 // ---------------------------------------------------------------- kernels
-template <int D>
-__global__ __launch_bounds__(kThreads) void moda_page_select_kernel(SelectParams p) {
-  __shared__ u64 keys[kChunk];
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void moda_page_select_kernel(SelectParams p) {
+  constexpr int kWaves = THREADS / 64;
+  __shared__ u64 keys[Choice<THREADS>::kChunk];
   __shared__ __attribute__((aligned(16))) double sums[2 * D];
-  __shared__ Choice c;
+  __shared__ Choice<THREADS> c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.x / p.Hk, g = blockIdx.x - b * p.Hk, n = pages_filled(p, b);
   choice_start(c);
@@ -274,10 +281,10 @@ __global__ __launch_bounds__(kThreads) void moda_page_select_kernel(SelectParams
   Seen seen;
   const bool choice = n > p.keep;  // (uniform; else all pages that there are)
   if (choice && first < n) s.load(p, first);
-  if (choice) query_sums<D, kThreads>(p, b, g, sums);
+  if (choice) query_sums<D, THREADS>(p, b, g, sums);
   __syncthreads();
   if (!choice) {
-    for (int i = threadIdx.x; i < n; i += kThreads) seen.add(keys[i] = page_at(s.table, i, p.n_pages) < 0 ? 0ull : kStays);
+    for (int i = threadIdx.x; i < n; i += THREADS) seen.add(keys[i] = page_at(s.table, i, p.n_pages) < 0 ? 0ull : kStays);
   } else if (first < n) {  // (uniform over a wave)
     s.query(sums);
     while (true) {
@@ -315,14 +322,15 @@ __global__ __launch_bounds__(256) void moda_page_score_kernel(SelectParams p, in
     s.load(p, first);
   }
 }
-__global__ __launch_bounds__(kThreads) void moda_page_choose_kernel(SelectParams p) {
-  __shared__ Choice c;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void moda_page_choose_kernel(SelectParams p) {
+  __shared__ Choice<THREADS> c;
   const u64* keys = p.keys + (size_t)blockIdx.x * p.cols;
   const int n = pages_filled(p, blockIdx.x / p.Hk);
   choice_start(c);
   __syncthreads();
   Seen seen;
-  for (int i = threadIdx.x; i < n; i += kThreads) seen.add(keys[i]);
+  for (int i = threadIdx.x; i < n; i += THREADS) seen.add(keys[i]);
   seen.flush(c);
   __syncthreads();
   choose<false>(c, keys, n, p.keep, p.pages + (size_t)blockIdx.x * p.keep);
@@ -330,7 +338,19 @@ __global__ __launch_bounds__(kThreads) void moda_page_choose_kernel(SelectParams
 
 static int columns(const SelectParams& p) { return (int)(((long long)p.T + (1 << p.shift) - 1) >> p.shift); }
 
-static bool in_one(const SelectParams& p) { return columns(p) <= kChunk; }
+// How a choice is made: 0: two kernels, else one, a workgroup of so many threads per (sequence, key/value head).  1024 threads, which fill a compute
+// unit / 256, of which several share one / two kernels, us, (sequence, head)s, pages:
+//   d = 128   8, 60 6.2 / 5.7 / 7.8;   8, 180 - / 7.7 / 7.8;   8, 250 8.8 / 8.8 / 7.9;   8, 500 11.1 / 12.9 / 8.8;   8, 2000 25.3 / - / 10.1;   64, 500 11.1 / 12.9 / 9.3
+//             64, 2000 27.6 / - / 19.0;   128, 250 8.9 / 8.9 / 8.9;   128, 500 11.2 / 12.8 / 11.7;   128, 2000 28.7 / - / 27.4;   256, 250 9.3 / 9.2 / 11.4
+//             256, 1000 23.5 / 29.0 / 27.7;   256, 4000 86.6 / - / 104.6
+//             384, 120 12.9 / 8.0 / 12.6;   512, 1000 42.1 / 40.3 / 46.6;   1024, 250 38.1 / 22.6 / 33.2;   1024, 1000 92.9 / 87.2 / 111.6
+//   d = 64    8, 250 7.1 / 6.8 / 8.0;   8, 500 8.8 / 8.9 / 8.3;   128, 500 8.9 / 9.2 / 9.8;   128, 1000 11.3 / 13.3 / 13.2;   256, 1000 15.6 / 18.3 / 17.1;   1024, 1000 50.9 / 40.4 / 53.1
+static int threads_of_one(const SelectParams& p, int d) {
+  const int cols = columns(p);
+  const long long groups = (long long)p.B * p.Hk;
+  if ((long long)cols * d <= (groups > 64 ? 32000 : 24000) || (groups > 256 && cols <= Choice<256>::kChunk)) return 256;
+  return groups > 64 && cols <= Choice<1024>::kChunk ? 1024 : 0;
+}
 
 size_t select_workspace_bytes(const SelectParams& p) { return (size_t)p.B * p.Hk * columns(p) * sizeof(u64); }
 
@@ -338,9 +358,13 @@ hipError_t launch_select(SelectParams p, int d, void* workspace, hipStream_t str
   p.cols = columns(p);
   p.keys = (u64*)workspace;
   const long long groups = (long long)p.B * p.Hk;
-  if (!grid_ok(groups, kThreads)) return kGridTooLarge;
-  if (in_one(p))
-    return launch_kernel(d == 128 ? moda_page_select_kernel<128> : moda_page_select_kernel<64>, dim3((unsigned)groups), dim3(kThreads), stream, p);
+  if (!grid_ok(groups, 1024)) return kGridTooLarge;
+  const int threads = threads_of_one(p, d);
+  if (threads > 0) {
+    auto* kernel = d == 128 ? (threads == 256 ? moda_page_select_kernel<128, 256> : moda_page_select_kernel<128, 1024>)
+                            : (threads == 256 ? moda_page_select_kernel<64, 256> : moda_page_select_kernel<64, 1024>);
+    return launch_kernel(kernel, dim3((unsigned)groups), dim3(threads), stream, p);
+  }
   // a wave takes several batches of pages where there are more than 16 waves a compute unit
   const int per_batch = 8 * 256 / d;
   const long long all = groups * ((p.cols + per_batch - 1) / per_batch);
@@ -350,7 +374,9 @@ hipError_t launch_select(SelectParams p, int d, void* workspace, hipStream_t str
   const hipError_t e = launch_kernel(d == 128 ? moda_page_score_kernel<128> : moda_page_score_kernel<64>, dim3((unsigned)(groups * chunks)),
                                      dim3(256), stream, p, batches, chunks);
   if (e != hipSuccess) return e;
-  return launch_kernel(moda_page_choose_kernel, dim3((unsigned)groups), dim3(kThreads), stream, p);
+  // (250 pages of 8 heads, both kernels: 8.8 us with 1024 threads, 7.7 with 256)
+  const bool few = p.cols <= Choice<256>::kChunk;
+  return launch_kernel(few ? moda_page_choose_kernel<256> : moda_page_choose_kernel<1024>, dim3((unsigned)groups), dim3(few ? 256 : 1024), stream, p);
 }
 
 }  // namespace moda
