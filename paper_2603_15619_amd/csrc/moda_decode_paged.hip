@@ -4,8 +4,10 @@
 // The formulas are those of moda_decode_shared.hip: (m, l, unnormalised O) of disjoint sets of rows merge exactly, so the rows are cut into
 // slices over workgroups, whose states go to the workspace in fp32, and a second kernel merges them.
 // The cut is made on the device, from the lengths themselves: a paged cache's table is as wide as the longest sequence may become, and a
-// cut by that bound would leave most workgroups without rows.  Slices are of one size for all sequences (least, good: see
-// launch_decode_paged), so that sequences of any lengths fill the chip evenly; every workgroup adds up the lengths and finds its slice.
+// cut by that bound would leave most workgroups without rows.  Slices are of about one size for all sequences, so that sequences of any lengths
+// fill the chip evenly; every workgroup adds up the lengths and finds its slice (find_slice).
+// What bounds it: long calls the reads (8 x 65536 ragged rows, 16 heads, d = 128 6.45 TB/s; 32 x 16000 8-bit rows, 64 heads on 8 5.3), short ones the chain of
+// three loads (lengths, page numbers, rows), each of about 0.8 us, and a second launch where a sequence has several slices (4 us).
 #include <algorithm>
 
 #include "moda_decode_columns.h"
@@ -32,43 +34,95 @@ struct Slice {
   int first, n;     // the sequence's first slice, and how many it has
 };
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
-// Slice s of all slices; a wave's lanes look at a sequence each.
-__device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lane) {
-  long long total = 0;  // (thousands of rows would do 32 bits, a large batch of long ones not: 16 bits at a time)
-  int rows = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
-    total += ((long long)wave_sum(rows >> 16) << 16) + wave_sum(rows & 0xffff);
-  }
-  // rows of a slice with so many workgroups, in whole steps of 1 << least_shift
+// (thousands of rows would do 32 bits, a large batch of long sequences not: 16 bits at a time)
+__device__ __forceinline__ long long wave_sum_rows(int rows) { return ((long long)wave_sum(rows >> 16) << 16) + wave_sum(rows & 0xffff); }
+
+// Rows of a slice, in whole steps of 1 << least_shift, where all sequences together have `total`.
+__device__ __forceinline__ unsigned slice_rows(const PagedParams& p, long long total) {
   auto share = [&](int workgroups) {
     const long long n = total * p.units + workgroups - 1, step = 1ll << p.least_shift;
     return ((n / workgroups + step - 1) >> p.least_shift) << p.least_shift;
   };
   const long long once = max(share(kPgOnce), (long long)kPgOnceRows), many = max(share(kPgMany), (long long)p.good);
-  const unsigned per = (unsigned)max(min(share(kPgFew), min(once, many)), 1ll << p.least_shift);
-  Slice r;
-  r.b = -1;
-  int before = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {  // (uniform)
-    if (p.B > 64) rows = b0 + lane < p.B ? paged_rows(p, b0 + lane) : 0;
-    const int n = b0 + lane < p.B ? max((int)(((unsigned)rows + per - 1) / per), 1) : 0;
-    const int to = before + wave_scan(n);  // of this sequence and those before it
-    const unsigned long long behind = __builtin_amdgcn_ballot_w64(to > s);
-    if (behind) {  // (uniform)
-      const int i = __builtin_ctzll(behind);
-      r.b = b0 + i;
-      r.rows = __builtin_amdgcn_readlane(rows, i);
-      r.n = __builtin_amdgcn_readlane(n, i);
-      r.first = __builtin_amdgcn_readlane(to, i) - r.n;
-      // (as many slices, of the same size)
-      r.per = ((((unsigned)r.rows + r.n - 1) / (unsigned)r.n + (1u << p.least_shift) - 1) >> p.least_shift) << p.least_shift;
-      r.begin = min((s - r.first) * r.per, r.rows);
-      return r;
+  return (unsigned)max(min(share(kPgFew), min(once, many)), 1ll << p.least_shift);
+}
+// Slice s of the n slices, the first of them slice `first`, that sequence b of so many rows has.
+__device__ __forceinline__ Slice slice_of(const PagedParams& p, int s, int b, int rows, int first, int n) {
+  // (all of the same size)
+  const int per = ((((unsigned)rows + n - 1) / (unsigned)n + (1u << p.least_shift) - 1) >> p.least_shift) << p.least_shift;
+  return Slice{b, min((s - first) * per, rows), rows, per, first, n};
+}
+
+// Slice s of all slices.  Up to kPgLook sequences every wave looks at their lengths, a lane at one of each 64; more of them moda_paged_deal_kernel
+// has dealt the slices out.
+constexpr int kPgLook = 256;
+__device__ __forceinline__ Slice find_slice(const PagedParams& p, int s, int lane) {
+  if (p.B <= kPgLook) {  // (uniform)
+    constexpr int kChunks = kPgLook / 64;
+    int rows[kChunks];
+    long long total = 0;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) rows[i] = i * 64 + lane < p.B ? paged_rows(p, i * 64 + lane) : 0;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+      if (i * 64 < p.B) total += wave_sum_rows(rows[i]);
+    const unsigned per = slice_rows(p, total);
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (i * 64 >= p.B) break;  // (uniform)
+      const int n = i * 64 + lane < p.B ? max((int)(((unsigned)rows[i] + per - 1) / per), 1) : 0;
+      const int to = before + wave_scan(n);  // of this sequence and those before it
+      const unsigned long long behind = __builtin_amdgcn_ballot_w64(to > s);
+      if (behind) {  // (uniform)
+        const int l = __builtin_ctzll(behind), n_l = __builtin_amdgcn_readlane(n, l);
+        return slice_of(p, s, i * 64 + l, __builtin_amdgcn_readlane(rows[i], l), __builtin_amdgcn_readlane(to, l) - n_l, n_l);
+      }
+      before = __builtin_amdgcn_readlane(to, 63);
     }
-    before = __builtin_amdgcn_readlane(to, 63);
+    return Slice{-1, 0, 0, 0, 0, 0};
   }
-  return r;
+  // the last sequence whose first slice is s or one before it, among [b, end): 64 of them at a time
+  int b = 0, end = p.B;
+  while (end - b > 1) {  // (uniform)
+    const int step = (end - b + 63) / 64, i = b + lane * step;
+    const unsigned long long upto = __builtin_amdgcn_ballot_w64(i < end && p.ws_deal[2 * min(i, end - 1)] <= s);
+    b += (__builtin_popcountll(upto) - 1) * step;  // (the first of them is)
+    end = min(end, b + step);
+  }
+  const int first = __builtin_amdgcn_readfirstlane(p.ws_deal[2 * b]), n = __builtin_amdgcn_readfirstlane(p.ws_deal[2 * b + 1]);
+  if (s >= first + n) return Slice{-1, 0, 0, 0, 0, 0};
+  return slice_of(p, s, b, __builtin_amdgcn_readfirstlane(paged_rows(p, b)), first, n);
+}
+
+// Many sequences: first slice and number of slices of each, by one workgroup.
+constexpr int kDealThreads = 1024;
+__global__ __launch_bounds__(kDealThreads) void moda_paged_deal_kernel(PagedParams p) {
+  constexpr int kWaves = kDealThreads / 64;
+  __shared__ long long sums[kWaves];
+  __shared__ int counts[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  long long total = 0;
+  for (int b0 = 0; b0 < p.B; b0 += kDealThreads) total += wave_sum_rows(b0 + tid < p.B ? paged_rows(p, b0 + tid) : 0);
+  if (lane == 0) sums[wave] = total;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kWaves; ++w) total += sums[w];
+  const unsigned per = slice_rows(p, total);
+  int before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += kDealThreads) {  // (uniform)
+    const int b = b0 + tid, n = b < p.B ? max((int)(((unsigned)paged_rows(p, b) + per - 1) / per), 1) : 0, to = wave_scan(n);
+    if (lane == 63) counts[wave] = to;
+    __syncthreads();
+    const int of_wave = counts[lane % kWaves], up_to = row_scan(of_wave);
+    const int first = before + __builtin_amdgcn_readlane(up_to - of_wave, wave) + to - n;  // (with all lanes: one of them is read)
+    if (b < p.B) {
+      p.ws_deal[2 * b] = first;
+      p.ws_deal[2 * b + 1] = n;
+    }
+    before += __builtin_amdgcn_readlane(up_to, kWaves - 1);
+    __syncthreads();  // (the counts have been read)
+  }
 }
 
 // The one slice of sequence b.
@@ -199,7 +253,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
   const int b = x.b, G = p.Hq / p.Hk, g = unit % p.Hk, gc = unit / p.Hk;
   const int nh = min(GT, G - gc * GT);
   const size_t bh = (size_t)b * p.Hq + g * G + gc * GT;
-  if (unit == 0 && s == x.first && tid == 0 && !p.single) {
+  if (unit == 0 && s == x.first && tid == 0 && !p.single && p.B <= kPgLook) {
     p.ws_deal[2 * b] = x.first;
     p.ws_deal[2 * b + 1] = x.n;
   }
@@ -385,7 +439,7 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
   const int b = x.b, G = p.Hq / p.Hk, g = unit % p.Hk, gc = unit / p.Hk;
   const int nh = min(kMatrixHeads, G - gc * kMatrixHeads);
   const size_t bh = (size_t)b * p.Hq + g * G + gc * kMatrixHeads;
-  if (unit == 0 && s == x.first && tid == 0 && !p.single) {
+  if (unit == 0 && s == x.first && tid == 0 && !p.single && p.B <= kPgLook) {
     p.ws_deal[2 * b] = x.first;
     p.ws_deal[2 * b + 1] = x.n;
   }
@@ -544,7 +598,10 @@ static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
   const long long finish_blocks = (heads + teams / by - 1) / (teams / by);
   if (!grid_ok(blocks, kPgWaves * 64) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
   auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX> : moda_paged_matrix_kernel<D, MX>;
-  const hipError_t e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kPgWaves * 64), stream, p);
+  hipError_t e = hipSuccess;
+  if (!p.single && p.B > kPgLook) e = launch_kernel(moda_paged_deal_kernel, dim3(1), dim3(kDealThreads), stream, p);
+  if (e != hipSuccess) return e;
+  e = launch_kernel(kernel, dim3((unsigned)blocks), dim3(kPgWaves * 64), stream, p);
   if (e != hipSuccess || p.single) return e;
   return launch_kernel(moda_paged_finish_kernel<D>, dim3((unsigned)finish_blocks), dim3(256), stream, p, by);
 }

@@ -87,6 +87,17 @@ def test_many_sequences(G, d, mx):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B", [64, 65, 200, 256, 257, 1000, 1500])
+@pytest.mark.parametrize("G,d,mx", [(1, 64, False), (8, 64, True)])
+def test_batches_around_what_a_wave_looks_at(B, G, d, mx):
+    """Short sequences, a few longer than one workgroup takes, empty ones at both ends; the table is wide, so that no sequence is known to be short."""
+    lens = [(i * 37) % 50 for i in range(B)]
+    lens[0], lens[1], lens[B // 2], lens[B - 2], lens[B - 1] = 0, 3000, 1300, 2100, 0
+    check(G, 1, 16, d, lens, L=1, mx=mx, max_pages=200, seed=B)
+    check(G, 1, 16, d, [0] * B, L=1, mx=mx, max_pages=200, seed=B)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("G", [1, 4, 12])
 def test_lengths_out_of_range_and_bounds(G):
     check(G, 2, 16, 64, [100, -5, 1 << 30, 77], T=90, max_pages=7, L=3)   # below zero counts as zero, above T as T
