@@ -553,15 +553,18 @@ __global__ __launch_bounds__(256) void moda_paged_finish_kernel(PagedParams p, i
 // Rows that a sequence may have: the lengths themselves are on the device.
 static long long rows_bound(const PagedParams& p) { return p.selected ? (long long)p.n_selected << p.shift : p.T; }
 
-// Sequences of one slice each need no second kernel: where they are short, and longer ones where they fill the chip anyway.  Two kernels / one,
-// us, (batch x key/value heads), rows:
-//   bf16, d = 128   1 head   8, 100 7.8 / 4.6;   64, 400 8.6 / 7.4;   8, 700 8.1 / 9.8;   512, 1000 39.5 / 36.2;   8 heads   64, 100 11.1 / 6.8;   8, 400 10.7 / 10.3;
-//                   8, 700 10.6 / 12.5;   512, 1000 49.6 / 39.2
-//   bf16, d = 64    1 head   8, 700 8.1 / 6.7;   8, 1000 8.1 / 7.9;   4 heads   8, 700 9.9 / 8.8;   8, 1000 10.1 / 10.2
-//   8 bits, d = 128   1 head   8, 400 8.3 / 6.9;   8, 700 8.5 / 8.6;   8 heads   8, 400 11.7 / 10.6;   8, 700 11.7 / 13.2;   d = 64   1 head   8, 1000 8.6 / 6.9;   4 heads   8, 1000 10.3 / 11.0
+// Sequences of one slice each need no second kernel: where they are short, and longer ones where they fill half the chip or all of it anyway.  Two
+// kernels / one, us, (batch x key/value heads), rows:
+//   bf16, d = 128   1 head   8, 100 7.8 / 4.6;   64, 400 8.6 / 7.4;   8, 700 8.1 / 9.8;   128, 700 13.7 / 12.4;   128, 1000 16.5 / 17.2;   256, 1000 22.1 / 19.7
+//                   8 heads   64, 100 11.1 / 6.8;   8, 400 10.7 / 10.3;   8, 700 10.6 / 12.5;   512, 1000 49.6 / 39.2
+//   bf16, d = 64    1 head   8, 700 8.1 / 6.7;   8, 1000 8.1 / 7.9;   128, 1500 12.8 / 13.4;   256, 2000 21.7 / 20.3;   4 heads   8, 700 9.9 / 8.8;   8, 1000 10.1 / 10.2
+//   8 bits, d = 128   1 head   8, 400 8.3 / 6.9;   8, 700 8.5 / 8.6;   128, 1000 12.3 / 11.9;   256, 1500 20.2 / 18.9;   8 heads   8, 400 11.7 / 10.6;   8, 700 11.7 / 13.2
+//   8 bits, d = 64    1 head   8, 1000 8.6 / 6.9;   256, 2000 15.5 / 14.1;   4 heads   8, 1000 10.3 / 11.0
+// (16 waves for one short sequence: 8 x 400 rows of d = 128 7.4 -> 6.9, 8 x 100 4.3 -> 5.5: not built.)
 static bool in_one(const PagedParams& p, int d, bool mx) {
-  const long long rows = rows_bound(p);
-  return rows * d <= (mx && p.heads_per <= 2 ? 80000 : 53000) || (rows <= 1024 && (long long)p.B * p.units >= 256);
+  const long long channels = rows_bound(p) * d, groups = (long long)p.B * p.units;
+  const long long alone = mx && p.heads_per <= 2 ? 80000 : 53000;
+  return channels <= (groups >= 256 ? 160000 : groups >= 128 ? alone * 3 / 2 : alone);
 }
 
 // Slices of all sequences together that find_slice makes of at most so many rows: one of every sequence and as many as have its size.
