@@ -44,7 +44,8 @@ __device__ __forceinline__ unsigned slice_rows(const PagedParams& p, long long t
     return ((n / workgroups + step - 1) >> p.least_shift) << p.least_shift;
   };
   const long long once = max(share(kPgOnce), (long long)kPgOnceRows), many = max(share(kPgMany), (long long)p.good);
-  return (unsigned)max(min(share(kPgFew), min(once, many)), 1ll << p.least_shift);
+  // (2^30 rows: more than a sequence has)
+  return (unsigned)min(max(min(share(kPgFew), min(once, many)), 1ll << p.least_shift), 1ll << 30);
 }
 // Slice s of the n slices, the first of them slice `first`, that sequence b of so many rows has.
 __device__ __forceinline__ Slice slice_of(const PagedParams& p, int s, int b, int rows, int first, int n) {
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
       }
     }
   }
-  if (s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice
+  if (p.depth_count > 0 && s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice
     const size_t at = ((size_t)b * p.Hk + g) * p.depth_alloc * RB;
     const __amdgpu_buffer_rsrc_t kb = rows_buffer(p.Kd + at, p.depth_count * RB), vb = rows_buffer(p.Vd + at, p.depth_count * RB);
     constexpr int W = CPL / 8;  // 16-byte pieces of a lane's channels
@@ -464,7 +465,7 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
     list = PageList(p, b, g);
     list.fetch(p, (x.begin + first) >> p.shift, lane);
   }
-  if (s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice, first
+  if (p.depth_count > 0 && s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice, first
     int first;
     const int n_slots = part(p.depth_count, first);
     const size_t at = ((size_t)b * p.Hk + g) * p.depth_alloc * RB + (size_t)first * RB;
