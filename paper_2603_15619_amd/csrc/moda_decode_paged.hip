@@ -341,6 +341,147 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
 }
 
 // ---------------------------------------------------------------- rows on the matrix pipe
+// Up to COLS query heads of a group are the columns of S^T = K Q^T and O^T += V^T P^T, a wave folds 32 rows at a time.  32 columns: Columns (moda_decode_columns.h).
+// 16 columns, with the 16 x 16 x 32 products: lane l holds column l % 16; S^T of rows 16 t + 4 (l / 16) + j in s[t][j], which packed to bf16 is the
+// second operand of the product over rows if that takes the rows in the same order; O^T of channels 16 cb + 4 (l / 16) + j.
+template <int D>
+struct Columns16 {
+  using Tl = Tile<D>;
+  static constexpr int kSteps = D / 32, kBlocks = D / 16;
+  bf16x8 q[kSteps];
+  f32x4 o[kBlocks];
+  float m, l;
+  int row, tr;  // this lane's place in a tile: chunk l / 16 of row l % 16; its part of a transposing read
+  __device__ __forceinline__ void init(const char* q_row, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) q[st] = *(const bf16x8*)(q_row + st * 64 + g * 16);
+#pragma unroll
+    for (int cb = 0; cb < kBlocks; ++cb) o[cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+    row = Tl::off(i, g);
+    tr = Tl::off(g * 4 + (i >> 2), (i & 3) >> 1) + (i & 1) * 8;
+  }
+  // What the four lanes of a column hold, put together.
+  template <class F>
+  __device__ __forceinline__ static float over_column(float x, F&& f) {
+    const int i = __builtin_bit_cast(int, x);
+    auto r = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+    const int y = __builtin_bit_cast(int, f(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])));
+    auto h = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return f(__builtin_bit_cast(float, (int)h[0]), __builtin_bit_cast(float, (int)h[1]));
+  }
+  // 32 rows: K from LDS address `k`, V from `v`; `lower` of the first 16 and `upper` of the others count.
+  __device__ __forceinline__ void fold(unsigned k, unsigned v, int lane, int lower, int upper, float c2) {
+    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const unsigned x = (unsigned)xor_here((int)(row + k), st << 6);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8 __attribute__((address_space(3)))*)(size_t)(x + t * 16 * Tl::kRowBytes), q[st], s[t],
+                                                       0, 0, 0);
+    }
+    if (min(lower, upper) < 16) {  // (uniform)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((lane >> 4) * 4 + j >= (t == 0 ? lower : upper)) s[t][j] = -INFINITY;
+    }
+    float bm = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bm = fmaxf(bm, s[t][j]);
+    bm = over_column(bm, [](float a, float b) { return fmaxf(a, b); });
+    // (the reference as in Columns: raised when the maximum exceeds it by more than 8 powers of two)
+    const bool raise = bm > m + 8.0f / c2 || m == -INFINITY;
+    if (__builtin_amdgcn_ballot_w64(raise) != 0) {  // (uniform)
+      const float mn = raise ? bm : m;
+      const float al = mn == m ? 1.f : fast_exp2((m - mn) * c2);
+      m = mn;
+      l *= al;
+#pragma unroll
+      for (int cb = 0; cb < kBlocks; ++cb)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[cb][j] *= al;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c2;
+    float pv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      pv[i] = fast_exp2(s[i >> 2][i & 3] * c2 - mc);
+      l += pv[i];
+    }
+    const bf16x8 pb = pack8(pv);  // (rounded as in Columns)
+#pragma unroll
+    for (int cb = 0; cb < kBlocks; ++cb) {
+      const unsigned x = (unsigned)xor_here((int)(tr + v), cb << 5);
+      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(size_t)x);
+      const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(size_t)(x + 16 * Tl::kRowBytes));
+      o[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7)), pb, o[cb], 0, 0, 0);
+    }
+  }
+  // The states of the workgroup's waves folded, the first n columns to put(column, piece of four channels, sums, (reference, normaliser)).  LDS: piece c of
+  // column q at 16 c + (q ^ c % 16), in units of 16 bytes, of the wave's part.
+  template <class Put>
+  __device__ __forceinline__ void finish(unsigned char* smem, float (*stat)[32][2], float c2, int lane, int wave, int n, Put&& put) const {
+    constexpr int kPieces = D / 4, kPart = 16 * D * 4;
+    const int i16 = lane & 15, g = lane >> 4;
+    const float l_all = over_column(l, [](float a, float b) { return a + b; });
+    __syncthreads();  // (the tiles are not read any more)
+#pragma unroll
+    for (int cb = 0; cb < kBlocks; ++cb) {
+      const int piece = cb * 4 + g;
+      *(f32x4*)(smem + wave * kPart + (piece * 16 + (i16 ^ (piece & 15))) * 16) = o[cb];
+    }
+    if (g == 0) {
+      stat[wave][i16][0] = m;
+      stat[wave][i16][1] = l_all;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = threadIdx.x; i < 16 * kPieces; i += kShWaves * 64) {
+      const int q = i / kPieces, piece = i % kPieces;
+      if (q >= n) continue;
+      float mm = -INFINITY, ll = 0.f;
+      f32x4 oo = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kShWaves; ++w) mm = fmaxf(mm, stat[w][q][0]);
+#pragma unroll
+      for (int w = 0; w < kShWaves; ++w) {
+        const float f = stat[w][q][0] == -INFINITY ? 0.f : fast_exp2((stat[w][q][0] - mm) * c2);
+        ll += f * stat[w][q][1];
+        const f32x4 x = *(const f32x4*)(smem + w * kPart + (piece * 16 + (q ^ (piece & 15))) * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) oo[j] += f * x[j];
+      }
+      put(q, piece, oo, (f32x2){mm, ll});
+    }
+  }
+};
+template <int D>
+struct Columns32 : Columns<D> {
+  FragAddr<D> fa;
+  __device__ __forceinline__ void init(const char* q_row, int lane) {
+    Columns<D>::init(q_row, lane >> 5);
+    fa.init(lane);
+  }
+  __device__ __forceinline__ void fold(unsigned k, unsigned v, int lane, int lower, int upper, float c2) {
+    Columns<D>::template fold<1, true>(k, v, fa, lane, lower, c2, nullptr, 0, 0, upper);
+  }
+  template <class Put>
+  __device__ __forceinline__ void finish(unsigned char* smem, float (*stat)[32][2], float c2, int, int, int n, Put&& put) const {
+    fold_waves<D, 1>(*this, smem, stat, c2, n, nullptr, nullptr, put);
+  }
+};
+template <int D, int COLS>
+using ColumnsOf = std::conditional_t<COLS == 16, Columns16<D>, Columns32<D>>;
+
+__device__ __forceinline__ void lds_store(unsigned at, const u32x4& x) { *(u32x4 __attribute__((address_space(3)))*)(size_t)at = x; }
+
 // A block of 32 rows in flight: pieces of 1 KB of K and of V, and the scales of 8-bit rows.
 template <int D, bool MX>
 struct PageBlock {
@@ -350,23 +491,31 @@ struct PageBlock {
   int left[2];  // rows of the first and the other 16 that count
 };
 
+// bf16 rows: the chunk that a lane fetches of piece q is the one whose place in the tile it fills: offset g_off ^ piece_xor(q) in the rows.
+template <int D>
+__device__ __forceinline__ int fetch_offset(int lane) {
+  const int row = lane / Tile<D>::kChunks;
+  return row * D * 2 + ((lane % Tile<D>::kChunks ^ Tile<D>::swz(row)) << 4);
+}
+template <int D>
+__device__ constexpr int fetch_xor(int q) {
+  return D == 128 ? (q & 3) << 4 : (q & 1) * 32;
+}
+
 // Every wave by itself: rows [first, first + n) of the list (first, and n unless the sequence ends, multiples of 32), 32 at a time through its two
-// LDS tiles at `lds`, kPF blocks in flight in registers.  8-bit rows become bf16 on the way to LDS, exactly: 32 conversions per lane and block
+// LDS tiles at `lds`, kPF blocks in flight in registers.  8-bit rows become bf16 on the way to LDS, exactly: 64 conversions per lane and block
 // (d = 128) beside 16 matrix instructions.
-template <int D, bool MX, int kPF>
-__device__ __forceinline__ void read_pages(Columns<D>& c, const PagedParams& p, PageList& list, int g, int first, int n, unsigned lds, float c2) {
+template <int D, bool MX, int kPF, class C>
+__device__ __forceinline__ void read_pages(C& c, const PagedParams& p, PageList& list, int g, int first, int n, unsigned lds, float c2) {
   using Tl = Tile<D>;
   using Block = PageBlock<D, MX>;
   constexpr int CB = MX ? D : 2 * D, SB = D / kBlock, kInst = Block::kInst, kRows = 32 / kInst, kHalf = 32 * Tl::kRowBytes;
   constexpr int LPR = 64 / kRows;  // lanes of a row
   const int lane = threadIdx.x & 63, jr = lane / LPR, pc = lane % LPR;
-  FragAddr<D> fa;
-  fa.init(lane);
-  // bf16: the chunk that a lane fetches is the one whose place in the tile it fills; 8 bits: its two chunks go to their places
-  const int g_off = MX ? jr * CB + pc * 16 : jr * CB + ((pc ^ Tl::swz(jr)) << 4);
+  // (8 bits: a lane's two chunks of bf16 go to their places, which differ in one bit)
+  const int g_off = MX ? jr * CB + pc * 16 : fetch_offset<D>(lane);
   const int s_off = jr * SB + pc / 2;
   const unsigned to = MX ? lds + jr * Tl::kRowBytes + (((2 * pc) ^ Tl::swz(jr)) << 4) : lds + lane * 16;
-  auto piece_xor = [](int q) { return D == 128 ? (MX ? (q & 1) * 32 : (q & 3) << 4) : (MX ? 0 : (q & 1) * 32); };
   const int n_blocks = (n + 31) / 32;
   auto issue = [&](int blk, Block& r) {
     const int row = first + blk * 32;
@@ -381,7 +530,7 @@ __device__ __forceinline__ void read_pages(Columns<D>& c, const PagedParams& p, 
 #pragma unroll
       for (int q = h * kInst / 2; q < (h + 1) * kInst / 2; ++q) {
         const int at_row = slot + q * kRows - h * 16;
-        const int v_off = MX ? g_off : xor_here(g_off, piece_xor(q));
+        const int v_off = MX ? g_off : xor_here(g_off, fetch_xor<D>(q));
         r.k[q] = __builtin_amdgcn_raw_buffer_load_b128(kb, v_off, at_row * CB, 2);
         r.v[q] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off, at_row * CB, 2);
       }
@@ -396,17 +545,16 @@ __device__ __forceinline__ void read_pages(Columns<D>& c, const PagedParams& p, 
       }
     }
   };
-  auto store = [&](unsigned at, const u32x4& x) { *(u32x4 __attribute__((address_space(3)))*)(size_t)at = x; };
   auto stage = [&](const u32x4 (&x)[kInst], const unsigned (&s)[MX ? kInst : 1], int tile) {
 #pragma unroll
     for (int q = 0; q < kInst; ++q) {
       if (MX) {
         const float sc = scale_of(s[q]);
-        const unsigned at = (unsigned)xor_here((int)(to + tile), piece_xor(q)) + q * kRows * Tl::kRowBytes;
-        store(at, (u32x4){codes_bf16<false>(x[q][0], sc), codes_bf16<true>(x[q][0], sc), codes_bf16<false>(x[q][1], sc), codes_bf16<true>(x[q][1], sc)});
-        store(at ^ 16, (u32x4){codes_bf16<false>(x[q][2], sc), codes_bf16<true>(x[q][2], sc), codes_bf16<false>(x[q][3], sc), codes_bf16<true>(x[q][3], sc)});
+        const unsigned at = (unsigned)xor_here((int)(to + tile), D == 128 ? (q & 1) * 32 : 0) + q * kRows * Tl::kRowBytes;
+        lds_store(at, (u32x4){codes_bf16<false>(x[q][0], sc), codes_bf16<true>(x[q][0], sc), codes_bf16<false>(x[q][1], sc), codes_bf16<true>(x[q][1], sc)});
+        lds_store(at ^ 16, (u32x4){codes_bf16<false>(x[q][2], sc), codes_bf16<true>(x[q][2], sc), codes_bf16<false>(x[q][3], sc), codes_bf16<true>(x[q][3], sc)});
       } else {
-        store(to + tile + q * 1024, x[q]);
+        lds_store(to + tile + q * 1024, x[q]);
       }
     }
   };
@@ -422,18 +570,40 @@ __device__ __forceinline__ void read_pages(Columns<D>& c, const PagedParams& p, 
       stage(buf[i].v, buf[i].vs, kHalf);
       issue(blk + kPF, buf[i]);
       if (max(lower, upper) > 0)  // (uniform)
-        c.template fold<1, true>(lds, lds + kHalf, fa, lane, lower, c2, nullptr, 0, 0, upper);
+        c.fold(lds, lds + kHalf, lane, lower, upper, c2);
     }
   }
 }
 
-constexpr int kMatrixHeads = 32;
-template <int D, bool MX>
+// The same for n rows of bf16 that lie together (slots).
+template <int D, class C>
+__device__ __forceinline__ void read_together(C& c, const char* K, const char* V, int n, unsigned lds, float c2) {
+  constexpr int RB = D * 2, kInst = 32 * RB / 1024, kRows = 32 / kInst, kHalf = 32 * RB;
+  const int lane = threadIdx.x & 63, g_off = fetch_offset<D>(lane);
+  const __amdgpu_buffer_rsrc_t kb = rows_buffer(K, n * RB), vb = rows_buffer(V, n * RB);
+  for (int row = 0; row < n; row += 32) {
+    u32x4 k[kInst], v[kInst];
+#pragma unroll
+    for (int q = 0; q < kInst; ++q) {
+      const int v_off = xor_here(g_off, fetch_xor<D>(q));
+      k[q] = __builtin_amdgcn_raw_buffer_load_b128(kb, v_off, (row + q * kRows) * RB, 0);
+      v[q] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off, (row + q * kRows) * RB, 0);
+    }
+#pragma unroll
+    for (int q = 0; q < kInst; ++q) {
+      lds_store(lds + q * 1024 + lane * 16, k[q]);
+      lds_store(lds + kHalf + q * 1024 + lane * 16, v[q]);
+    }
+    c.fold(lds, lds + kHalf, lane, n - row, n - row - 16, c2);
+  }
+}
+
+template <int D, bool MX, int COLS>
 __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(PagedParams p) {
   constexpr int RB = D * 2, kPF = D == 128 && !MX ? 1 : 2;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kShWaves * 2 * 32 * RB];
   __shared__ float stat[kShWaves][32][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hi = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const unsigned lds = (unsigned)(size_t)(lds_ptr)smem + wave * 2 * 32 * RB;
   const float c2 = p.scale_log2;
   const int unit = blockIdx.x % p.units, s = blockIdx.x / p.units;
@@ -445,14 +615,14 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
   const Slice x = p.single ? whole_sequence(p, s) : find_slice(p, s, lane);
   if (x.b < 0) return;  // (uniform)
   const int b = x.b;
-  const int nh = min(kMatrixHeads, G - gc * kMatrixHeads);
-  const size_t bh = (size_t)b * p.Hq + g * G + gc * kMatrixHeads;
+  const int nh = min(COLS, G - gc * COLS);
+  const size_t bh = (size_t)b * p.Hq + g * G + gc * COLS;
   if (unit == 0 && s == x.first && tid == 0 && !p.single && p.B <= kPgLook) {
     p.ws_deal[2 * b] = x.first;
     p.ws_deal[2 * b + 1] = x.n;
   }
-  Columns<D> c;
-  c.init((const char*)p.Q + (bh + min(l32, nh - 1)) * RB, hi);
+  ColumnsOf<D, COLS> c;
+  c.init((const char*)p.Q + (bh + min(lane % COLS, nh - 1)) * RB, lane);  // (a column past the last repeats it and is not stored)
   // a wave's part of n rows: a quarter, in whole blocks of 32
   auto part = [&](int n, int& first) {
     const int q = ((n + kShWaves - 1) / kShWaves + 31) / 32 * 32;
@@ -466,18 +636,18 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
     list.fetch(p, (x.begin + first) >> p.shift, lane);
   }
   if (p.depth_count > 0 && s == x.first + x.n - 1) {  // (uniform) the slots go with the sequence's last slice, first
-    int first;
-    const int n_slots = part(p.depth_count, first);
-    const size_t at = ((size_t)b * p.Hk + g) * p.depth_alloc * RB + (size_t)first * RB;
-    read_by_wave<D, 1>(c, Rows{p.Kd + at, p.Vd + at, n_slots, nullptr, nullptr, 0}, lds, c2);
+    int slot;
+    const int n_slots = part(p.depth_count, slot);
+    const size_t at = (((size_t)b * p.Hk + g) * p.depth_alloc + slot) * RB;
+    read_together<D>(c, p.Kd + at, p.Vd + at, n_slots, lds, c2);
   }
   if (n > 0) {  // (uniform)
     list.len = filled(p.lengths, b, p.T);
     list.settle(p);
     read_pages<D, MX, kPF>(c, p, list, g, x.begin + first, n, lds, c2);
   }
-  const size_t to = (size_t)s * p.Hq + g * G + gc * kMatrixHeads;
-  fold_waves<D, 1>(c, smem, stat, c2, nh, nullptr, nullptr, [&](int j, int piece, const f32x4& o, const f32x2& ml) {
+  const size_t to = (size_t)s * p.Hq + g * G + gc * COLS;
+  c.finish(smem, stat, c2, lane, wave, nh, [&](int j, int piece, const f32x4& o, const f32x2& ml) {
     if (p.single) {  // (uniform)
       const bool none = ml[1] == 0.f;  // nothing seen, or nothing that has weight
       const float inv = none ? 0.f : 1.f / ml[1];
@@ -587,7 +757,7 @@ static int most_slices(const PagedParams& p, long long rows) {
 
 static void plan(PagedParams& p, int d, bool mx) {
   const int G = p.Hq / p.Hk;
-  p.heads_per = G <= 2 ? G : kMatrixHeads;
+  p.heads_per = G <= 2 ? G : G <= 16 ? 16 : 32;
   p.units = p.Hk * ((G + p.heads_per - 1) / p.heads_per);
   const int least = G <= 2 ? kPgWaves * 4 * 64 * (mx ? 16 : 8) / d : kShWaves * 32;  // what the waves take at a time: 64 to 256
   p.least_shift = __builtin_ctz(least);
@@ -612,7 +782,8 @@ static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
   while (by < teams && (long long)by * 4 * p.B < p.n_slices) by *= 2;
   const long long finish_blocks = (heads + teams / by - 1) / (teams / by);
   if (!grid_ok(blocks, kPgWaves * 64) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
-  auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX> : moda_paged_matrix_kernel<D, MX>;
+  auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX>
+                 : p.heads_per == 16 ? moda_paged_matrix_kernel<D, MX, 16> : moda_paged_matrix_kernel<D, MX, 32>;
   hipError_t e = hipSuccess;
   if (!p.single && p.B > kPgLook) e = launch_kernel(moda_paged_deal_kernel, dim3(1), dim3(kDealThreads), stream, p);
   if (e != hipSuccess) return e;
