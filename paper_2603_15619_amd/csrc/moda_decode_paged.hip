@@ -738,15 +738,21 @@ static long long rows_bound(const PagedParams& p) { return p.selected ? (long lo
 // Sequences of one slice each need no second kernel: where they are short, and longer ones where they fill half the chip or all of it anyway.  Two
 // kernels / one, us, (batch x key/value heads), rows:
 //   bf16, d = 128   1 head   8, 100 7.8 / 4.6;   64, 400 8.6 / 7.4;   8, 700 8.1 / 9.8;   128, 700 13.7 / 12.4;   128, 1000 16.5 / 17.2;   256, 1000 22.1 / 19.7
-//                   8 heads   64, 100 11.1 / 6.8;   8, 400 10.7 / 10.3;   8, 700 10.6 / 12.5;   512, 1000 49.6 / 39.2
-//   bf16, d = 64    1 head   8, 700 8.1 / 6.7;   8, 1000 8.1 / 7.9;   128, 1500 12.8 / 13.4;   256, 2000 21.7 / 20.3;   4 heads   8, 700 9.9 / 8.8;   8, 1000 10.1 / 10.2
-//   8 bits, d = 128   1 head   8, 400 8.3 / 6.9;   8, 700 8.5 / 8.6;   128, 1000 12.3 / 11.9;   256, 1500 20.2 / 18.9;   8 heads   8, 400 11.7 / 10.6;   8, 700 11.7 / 13.2
-//   8 bits, d = 64    1 head   8, 1000 8.6 / 6.9;   256, 2000 15.5 / 14.1;   4 heads   8, 1000 10.3 / 11.0
-// (16 waves for one short sequence: 8 x 400 rows of d = 128 7.4 -> 6.9, 8 x 100 4.3 -> 5.5: not built.)
+//                   8 heads   64, 100 9.6 / 5.9;   8, 400 9.5 / 8.1;   8, 700 9.5 / 9.9;   128, 700 13.5 / 11.7;   512, 1000 46.9 / 37.0
+//   bf16, d = 64    1 head   8, 700 8.1 / 6.7;   8, 1000 8.1 / 7.9;   128, 1500 12.8 / 13.4;   256, 2000 21.7 / 20.3;   8 heads   8, 700 9.6 / 8.3;   8, 1000 9.6 / 9.4
+//   8 bits, d = 128   1 head   8, 400 8.3 / 6.9;   8, 700 8.5 / 8.6;   128, 1000 12.3 / 11.9;   256, 1500 20.2 / 18.9;   8 heads   8, 400 10.6 / 8.8;   8, 700 10.7 / 10.6
+//   8 bits, d = 64    1 head   8, 1000 8.6 / 6.9;   256, 2000 15.5 / 14.1;   8 heads   8, 1000 9.7 / 9.3;   256, 2000 19.8 / 15.5
+// Lists are as long as each other, and so are the workgroups' times: there one kernel does for any length, where the groups are about a multiple of the
+// compute units.  The same for rows that lists name:
+//   bf16, d = 128, 8 heads   256, 2812 62.8 / 56.4;   448, 2812 108.4 / 98.1;   512, 11250 467 / 438;   640, 2812 152.3 / 144.5;   but 288, 2812 76.3 / 83.1;   576, 11250 526 / 540
+//   8 bits, d = 128, 8 heads   512, 2812 75.2 / 63.4;   1 head   512, 2812 65.3 / 60.5;   640, 2812 80.5 / 80.6;   768, 5625 182.1 / 177.1;   but 320, 5625 83.0 / 86.5
+// (Sequences of their own lengths, down to a tenth of the longest: 512, 2812 of bf16 77.4 / 75.2 and, one head, 67.8 / 74.1; 8 bits 51.8 / 45.7 and 40.4 / 43.4.
+// 16 waves for one short sequence: 8 x 400 rows of d = 128 7.4 -> 6.9, 8 x 100 4.3 -> 5.5: not built.)
 static bool in_one(const PagedParams& p, int d, bool mx) {
   const long long channels = rows_bound(p) * d, groups = (long long)p.B * p.units;
-  const long long alone = mx && p.heads_per <= 2 ? 80000 : 53000;
-  return channels <= (groups >= 256 ? 160000 : groups >= 128 ? alone * 3 / 2 : alone);
+  const long long alone = mx && p.heads_per <= 2 ? 80000 : 53000, units = 256, filled_units = (groups + units - 1) / units * units;
+  if (p.selected && groups >= units && groups * 6 >= filled_units * 5) return true;
+  return channels <= (groups >= units ? 160000 : groups * 2 >= units ? alone * 3 / 2 : alone);
 }
 
 // Slices of all sequences together that find_slice makes of at most so many rows: one of every sequence and as many as have its size.
@@ -763,7 +769,9 @@ static void plan(PagedParams& p, int d, bool mx) {
   p.least_shift = __builtin_ctz(least);
   // Rows of a slice in several rounds (us, rows / heads per group; 512 workgroups / 2048 of 512 rows or more / 2048 of 2048 or more):
   //   vector ALUs    8 x 65536 rows, 16 heads, d = 128: 577 / 525 / 525;  4 x 16000, 16 heads 74.8 / 69.4 / 74.9;  32 x 4000 8-bit, 8 heads 42.0 / 40.2 / 42.3
-  //   matrix pipe    32 x 16000 8-bit, 64 heads on 8, d = 128: 120.5 / 121.2 / 112.8;  64 x 16000 bf16 538 / 505 / 504;  4 x 30000, 64 on 4 39.2 / 45.6 / 40.5
+  //   matrix pipe, 2048 workgroups of 512 / 1024 / 2048 / 4096 rows or more, sequences down to a tenth of the longest: 32 x 16000 8-bit, 64 heads on 8, d = 128
+  //   116.5 / 116.1 / 108.7 / 116.0;  32 x 8000 bf16 103.9 / 101.4 / 107.0 / 100.2;  4 x 30000 bf16, 64 on 4 40.9 / 33.0 / 32.9 / 32.9;  16 x 8000 bf16, d = 64
+  //   31.5 / 32.6 / 34.1 / 34.0;  512 workgroups of any size 32 x 16000 8-bit, down to 0.7 of the longest: 179 against 162 / 162 / 165 / 157
   p.good = G <= 2 ? 512 : 2048;
   p.n_slices = most_slices(p, 1ll << 40);
 }

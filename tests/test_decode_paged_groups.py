@@ -81,3 +81,21 @@ def test_equal_heads_of_a_group(G):
     O, LSE = moda_attn_decode_paged(Q, **c.args(), lengths=ints([900, 31, 0]))
     O, LSE = O.view(3, 2, G, 64), LSE.view(3, 2, G)
     assert torch.equal(O, O[:, :, :1].expand_as(O)) and torch.equal(LSE, LSE[:, :, :1].expand_as(LSE))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G,Hk,B,d,mx", [(1, 8, 33, 64, False), (1, 2, 128, 128, True), (8, 16, 27, 64, True), (40, 4, 32, 64, False), (2, 1, 700, 64, False)])
+def test_lists_of_many_sequences(G, Hk, B, d, mx):
+    """Lists that many sequences have, longer than what short calls take, with sequences of nothing and of less than their list among them."""
+    rng = np.random.default_rng(B)
+    n, R = 180, 16
+    lens = [int(x) for x in rng.integers(0, 40 * R, B)]
+    lens[0], lens[1], lens[B - 1] = 200 * R, 0, 200 * R - 5
+    sel = np.full((B, Hk, n), -1, dtype=np.int32)
+    for b in range(B):
+        pages = -(-lens[b] // R)
+        for g in range(Hk):
+            some = np.sort(rng.permutation(pages)[:n])
+            sel[b, g, :len(some)] = some
+    sel[2, 0] = -1
+    check(G, Hk, R, d, lens, L=3, mx=mx, selected=sel, seed=B)
