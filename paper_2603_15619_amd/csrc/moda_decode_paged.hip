@@ -6,7 +6,7 @@
 // The cut is made on the device, from the lengths themselves: a paged cache's table is as wide as the longest sequence may become, and a
 // cut by that bound would leave most workgroups without rows.  Slices are of about one size for all sequences, so that sequences of any lengths
 // fill the chip evenly; every workgroup adds up the lengths and finds its slice (find_slice).
-// What bounds it: long calls the reads (8 x 65536 ragged rows, 16 heads, d = 128 6.45 TB/s; 32 x 16000 8-bit rows, 64 heads on 8 5.3), short ones the chain of
+// What bounds it: long calls the reads (8 x 65536 ragged rows, 16 heads, d = 128 6.45 TB/s; 32 x 16000 8-bit rows, 64 heads on 8 5.5), short ones the chain of
 // three loads (lengths, page numbers, rows), each of about 0.8 us, and a second launch where a sequence has several slices (4 us).
 #include <algorithm>
 
