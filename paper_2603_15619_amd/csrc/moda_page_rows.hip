@@ -43,7 +43,7 @@ __device__ __forceinline__ u32x2 quantise(const u32x4& x, unsigned& byte) {
   byte = max((int)((__builtin_bit_cast(unsigned, a) + 0x1fffffu) >> 23) - 8, kLeastByte);
   const float inv = scale_of(254 - byte), most = byte == kMostByte ? 240.f : 448.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_fmed3f(v[i] * inv, -most, most) + nan[i];
+  for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_fmed3f(v[i] * inv, -most, most) - nan[i];  // (-0 less 0 stays -0)
   u32x2 r;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
