@@ -395,7 +395,8 @@ moda_status moda_page_select(const void* Q, const void* Kbounds, const int32_t* 
  *   workspace: at least moda_attn_decode_paged_workspace_bytes(x, s) bytes, 16-byte aligned; does not depend on T
  * A token that sees nothing, or whose logits are all -inf, gets O = 0, LSE = -inf.  Uses Hq, T (bounds the lengths: one below 0 counts as 0, one
  * above T as T; max_pages * page_rows >= T >= 0), depth_alloc, depth_count and scale of the shape.  Logits, references, normalisers and
- * sums are fp32.
+ * sums are fp32.  The softmax weights that multiply the values are fp32 for groups of up to 4 heads (of 3 and 4: sums of two bf16 numbers, off by
+ * 2^-15 of themselves), rounded to bf16 for larger ones.
  */
 size_t moda_attn_decode_paged_workspace_bytes(const moda_pages* x, const moda_shape* s);
 moda_status moda_attn_decode_paged(const void* Q, const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales,

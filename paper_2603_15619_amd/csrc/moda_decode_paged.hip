@@ -344,7 +344,30 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
 // Up to COLS query heads of a group are the columns of S^T = K Q^T and O^T += V^T P^T, a wave folds 32 rows at a time.  32 columns: Columns (moda_decode_columns.h).
 // 16 columns, with the 16 x 16 x 32 products: lane l holds column l % 16; S^T of rows 16 t + 4 (l / 16) + j in s[t][j], which packed to bf16 is the
 // second operand of the product over rows if that takes the rows in the same order; O^T of channels 16 cb + 4 (l / 16) + j.
-template <int D>
+// Weights go into that product as bf16, rounded as in Columns, or (SPLIT) as sums of two bf16 numbers, a product each: groups of 3 and 4 heads, to which
+// moda_attn_decode gives fp32 weights, are off by O's own rounding alone here too, 0.0017 of their size on N(0,1) data instead of 0.0023.  (Rounded once /
+// split, us, sequences down to half of the longest: 64 x 2100 rows of d = 64, 32 heads on 8, 31.5 / 32.0;  32 x 8000 rows of d = 128, 32 on 8, 133.3 / 133.8;
+// 32 x 16000 8-bit rows, 32 on 8, 141.0 / 145.7.  More heads, whose weights moda_attn_decode rounds as well: 64 on 8 107.1 / 110.7, 256 on 8, 32 columns,
+// 167.8 / 176.4; there it is not done.)
+
+// Weights (0 or more) as sums of two bf16 numbers, off by 2^-15 of themselves: the largest below x, and the rest, rounded.  Both are above 0 where x is
+// (2^-102 or more), so that an infinite value stays one and does not become NaN.
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8& high, bf16x8& rest) {
+  u32x4 h;
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned a = __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, x[2 * i]), 1u);
+    const unsigned b = __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, x[2 * i + 1]), 1u);
+    h[i] = __builtin_amdgcn_perm(b, a, 0x07060302);  // the upper halves
+    r[2 * i] = x[2 * i] - bf16_hi(a);
+    r[2 * i + 1] = x[2 * i + 1] - bf16_hi(b);
+  }
+  high = __builtin_bit_cast(bf16x8, h);
+  rest = pack8(r);
+}
+
+template <int D, bool SPLIT>
 struct Columns16 {
   using Tl = Tile<D>;
   static constexpr int kSteps = D / 32, kBlocks = D / 16;
@@ -415,13 +438,17 @@ struct Columns16 {
       pv[i] = fast_exp2(s[i >> 2][i & 3] * c2 - mc);
       l += pv[i];
     }
-    const bf16x8 pb = pack8(pv);  // (rounded as in Columns)
+    bf16x8 pb, rest;
+    if constexpr (SPLIT) split8(pv, pb, rest);
+    else pb = pack8(pv);
 #pragma unroll
     for (int cb = 0; cb < kBlocks; ++cb) {
       const unsigned x = (unsigned)xor_here((int)(tr + v), cb << 5);
       const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(size_t)x);
       const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(size_t)(x + 16 * Tl::kRowBytes));
-      o[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7)), pb, o[cb], 0, 0, 0);
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      o[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb, o[cb], 0, 0, 0);
+      if constexpr (SPLIT) o[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, rest, o[cb], 0, 0, 0);
     }
   }
   // The states of the workgroup's waves folded, the first n columns to put(column, piece of four channels, sums, (reference, normaliser)).  LDS: piece c of
@@ -477,8 +504,8 @@ struct Columns32 : Columns<D> {
     fold_waves<D, 1>(*this, smem, stat, c2, n, nullptr, nullptr, put);
   }
 };
-template <int D, int COLS>
-using ColumnsOf = std::conditional_t<COLS == 16, Columns16<D>, Columns32<D>>;
+template <int D, int COLS, bool SPLIT>
+using ColumnsOf = std::conditional_t<COLS == 16, Columns16<D, SPLIT>, Columns32<D>>;
 
 __device__ __forceinline__ void lds_store(unsigned at, const u32x4& x) { *(u32x4 __attribute__((address_space(3)))*)(size_t)at = x; }
 
@@ -598,7 +625,7 @@ __device__ __forceinline__ void read_together(C& c, const char* K, const char* V
   }
 }
 
-template <int D, bool MX, int COLS>
+template <int D, bool MX, int COLS, bool SPLIT>
 __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(PagedParams p) {
   constexpr int RB = D * 2, kPF = D == 128 && !MX ? 1 : 2;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[kShWaves * 2 * 32 * RB];
@@ -621,7 +648,7 @@ __global__ __launch_bounds__(kShWaves * 64, 2) void moda_paged_matrix_kernel(Pag
     p.ws_deal[2 * b] = x.first;
     p.ws_deal[2 * b + 1] = x.n;
   }
-  ColumnsOf<D, COLS> c;
+  ColumnsOf<D, COLS, SPLIT> c;
   c.init((const char*)p.Q + (bh + min(lane % COLS, nh - 1)) * RB, lane);  // (a column past the last repeats it and is not stored)
   // a wave's part of n rows: a quarter, in whole blocks of 32
   auto part = [&](int n, int& first) {
@@ -791,7 +818,8 @@ static hipError_t launch_d(const PagedParams& p, hipStream_t stream) {
   const long long finish_blocks = (heads + teams / by - 1) / (teams / by);
   if (!grid_ok(blocks, kPgWaves * 64) || !grid_ok(finish_blocks, 256)) return kGridTooLarge;
   auto* kernel = p.heads_per == 1 ? moda_paged_slices_kernel<D, 1, MX> : p.heads_per == 2 ? moda_paged_slices_kernel<D, 2, MX>
-                 : p.heads_per == 16 ? moda_paged_matrix_kernel<D, MX, 16> : moda_paged_matrix_kernel<D, MX, 32>;
+                 : p.Hq / p.Hk <= 4 ? moda_paged_matrix_kernel<D, MX, 16, true>
+                 : p.heads_per == 16 ? moda_paged_matrix_kernel<D, MX, 16, false> : moda_paged_matrix_kernel<D, MX, 32, false>;
   hipError_t e = hipSuccess;
   if (!p.single && p.B > kPgLook) e = launch_kernel(moda_paged_deal_kernel, dim3(1), dim3(kDealThreads), stream, p);
   if (e != hipSuccess) return e;
