@@ -377,7 +377,8 @@ moda_status moda_page_read(const void* Kpages, const void* Vpages, const void* K
  *   in : Q [B, Hq, d]; Kbounds; page_table; lengths [B] or NULL (all T), read as for the decoding step
  *   out: pages [B, Hk, keep] int32: indices into the sequence's table, ascending, -1 behind the last
  *   workspace: at least moda_page_select_workspace_bytes(x, s) bytes (may be 0: then NULL is accepted), 16-byte aligned
- * keep >= 1, first, recent >= 0, first + recent <= keep.  Uses Hq and T of the shape: T bounds the lengths, max_pages * page_rows >= T >= 0.
+ * keep >= 1, first, recent >= 0, first + recent <= keep.  Uses Hq and T of the shape: T bounds the lengths, max_pages * page_rows >= T >= 0, and
+ * so decides the size of the workspace and, as for the decoding step below, the kernels: the least bound that holds is best.
  */
 size_t moda_page_select_workspace_bytes(const moda_pages* x, const moda_shape* s);
 moda_status moda_page_select(const void* Q, const void* Kbounds, const int32_t* page_table, const int32_t* lengths, int32_t* pages,
@@ -397,6 +398,9 @@ moda_status moda_page_select(const void* Q, const void* Kbounds, const int32_t* 
  * above T as T; max_pages * page_rows >= T >= 0), depth_alloc, depth_count and scale of the shape.  Logits, references, normalisers and
  * sums are fp32.  The softmax weights that multiply the values are fp32 for groups of up to 4 heads (of 3 and 4: sums of two bf16 numbers, off by
  * 2^-15 of themselves), rounded to bf16 for larger ones.
+ * The lengths are on the device, so it is T, or the lists' length, that decides how the step is made: where T rows are few, one kernel; else slices and a merge, also
+ * when the lengths turn out short (8 x 100 rows under a wide table: 8.1 us, with T = 100 4.9).  T is best the least bound that holds; a captured step
+ * keeps the one it was captured with.
  */
 size_t moda_attn_decode_paged_workspace_bytes(const moda_pages* x, const moda_shape* s);
 moda_status moda_attn_decode_paged(const void* Q, const void* Kpages, const void* Vpages, const void* Kscales, const void* Vscales,

@@ -624,7 +624,7 @@ def moda_page_select(Q, Kbounds, page_table, keep, page_rows, lengths=None, firs
     """pages [B,Hk,keep] (int32): for each (sequence, key/value head) the `first` first and `recent` last pages and those whose key bounds
     Kbounds [n_pages,Hk,2,d] promise the largest logits, summed over the heads of the group, for the queries Q [B,Hq,d]; indices into
     the sequence's row of page_table [B,max_pages], ascending, -1 behind the last.  lengths [B] (int32; None: T, None: all rows that the
-    table has).  What moda_attn_decode_paged takes as `selected`."""
+    table has); T bounds them, and decides the kernels and the workspace.  What moda_attn_decode_paged takes as `selected`."""
     if out is not None:
         r = (_native_module or _native()).page_select(Q, Kbounds, page_table, keep, page_rows, lengths, first, recent, T, out, workspace)
         if r is not None:
@@ -659,7 +659,7 @@ def moda_attn_decode_paged(Q, Kpages, Vpages, page_table, Kdepth=None, Vdepth=No
     """O [B,Hq,d], LSE [B,Hq] for one new token per sequence, under one softmax over the rows of its pages (moda_page_append has
     the cache's arguments; the token's own row is among them) and its depth slots Kdepth/Vdepth [B,Hk,depth_alloc,d] or None.
     lengths [B] (int32): the rows of each sequence; T bounds them (default: all rows that the table has) and is their number where lengths is
-    None.  selected [B,Hk,n] (int32): only the rows of these pages, indices into the sequence's row of page_table, each once, -1: none."""
+    None.  T also decides the kernels: under a table much wider than the sequences, a T of the longest length that may come is faster.  selected [B,Hk,n] (int32): only the rows of these pages, indices into the sequence's row of page_table, each once, -1: none."""
     r = (_native_module or _native()).paged(Q, Kpages, Vpages, page_table, Kdepth, Vdepth, lengths, selected, Kscales, Vscales, T,
                                             depth_count, scale, out, lse, workspace)
     if r is not None:
