@@ -763,12 +763,20 @@ __global__ __launch_bounds__(256) void moda_paged_finish_kernel(PagedParams p, i
 static long long rows_bound(const PagedParams& p) { return p.selected ? (long long)p.n_selected << p.shift : p.T; }
 
 // Sequences of one slice each need no second kernel: where they are short, and longer ones where they fill half the chip or all of it anyway.  Two
-// kernels / one, us, (batch x key/value heads), rows:
-//   bf16, d = 128   1 head   8, 100 7.8 / 4.6;   64, 400 8.6 / 7.4;   8, 700 8.1 / 9.8;   128, 700 13.7 / 12.4;   128, 1000 16.5 / 17.2;   256, 1000 22.1 / 19.7
-//                   8 heads   64, 100 9.6 / 5.9;   8, 400 9.5 / 8.1;   8, 700 9.5 / 9.9;   128, 700 13.5 / 11.7;   512, 1000 46.9 / 37.0
-//   bf16, d = 64    1 head   8, 700 8.1 / 6.7;   8, 1000 8.1 / 7.9;   128, 1500 12.8 / 13.4;   256, 2000 21.7 / 20.3;   8 heads   8, 700 9.6 / 8.3;   8, 1000 9.6 / 9.4
-//   8 bits, d = 128   1 head   8, 400 8.3 / 6.9;   8, 700 8.5 / 8.6;   128, 1000 12.3 / 11.9;   256, 1500 20.2 / 18.9;   8 heads   8, 400 10.6 / 8.8;   8, 700 10.7 / 10.6
-//   8 bits, d = 64    1 head   8, 1000 8.6 / 6.9;   256, 2000 15.5 / 14.1;   8 heads   8, 1000 9.7 / 9.3;   256, 2000 19.8 / 15.5
+// kernels / one, us, (batch x key/value heads), rows of the longest sequence: all as long, evenly down to half of it, down to a tenth of it (under 64 groups alike)
+//   bf16, d = 128, 1 head   8, 100 7.8 / 4.6;   8, 414 8.2 / 7.4;   8, 515 8.4 / 8.7;   64, 625 9.2 / 9.3, 9.7 / 9.3, 8.9 / 9.3
+//                    128, 625 12.0 / 11.7, 11.9 / 10.9, 10.7 / 9.3;   128, 781 13.9 / 14.6, 13.3 / 13.7, 11.1 / 11.4;   192, 937 19.5 / 17.9, 18.1 / 17.0, 16.0 / 16.1
+//                    256, 1250 29.1 / 25.9, 24.7 / 23.6, 19.4 / 22.0;   256, 1562 34.7 / 31.9, 28.9 / 28.9, 25.4 / 27.2;   512, 1250 53.7 / 49.1, 42.3 / 41.3, 33.1 / 34.1
+//   8 heads          8, 625 9.9 / 9.0;   8, 781 9.8 / 10.8;   128, 937 16.3 / 15.1, 17.1 / 14.0, 13.7 / 13.0;   128, 1562 23.1 / 22.1, 21.7 / 20.4, 19.1 / 19.7
+//                    256, 1562 38.1 / 32.3, 36.9 / 26.8, 27.0 / 22.7;   512, 1250 56.6 / 50.2, 51.5 / 41.8, 40.3 / 35.2
+//   8 bits, 1 head   8, 625 9.1 / 7.9;   8, 781 9.1 / 9.7;   128, 937 12.8 / 12.1, 13.1 / 11.7, 11.1 / 11.5;   256, 1562 22.6 / 21.3, 20.2 / 19.5, 18.0 / 18.2
+//   8 heads          8, 625 11.2 / 10.4;   8, 781 11.1 / 12.4;   128, 1250 18.0 / 15.8, 17.5 / 15.7, 17.1 / 15.6;   256, 1562 27.4 / 20.8, 27.3 / 20.0, 24.4 / 19.6
+//   bf16, d = 64     1 head   8, 828 8.3 / 7.5;   8, 1031 8.4 / 8.8;   128, 1250 13.0 / 12.1, 12.3 / 10.8, 10.9 / 9.5;   128, 1562 13.7 / 15.0, 13.1 / 14.0, 11.5 / 11.4
+//                    8 heads   8, 828 9.6 / 9.1;   8, 1031 9.6 / 10.5;   256, 2500 30.3 / 25.8, 27.0 / 22.3, 22.5 / 19.3
+// The limits are those of the form that crosses first, one head in bf16 (8-bit rows on the vector ALUs have their own below 256 groups).  From 256 groups on raggedness
+// decides: at the limit such sequences gain a ninth if all are as long and lose an eighth if they go down to a tenth.  Beyond the limits some forms
+// still gain, by up to a quarter (8 heads, 8 bits, 256 x 1562 rows; 192 groups of 8 heads and 1562 rows 33.6 / 25.0, 29.5 / 22.6, 22.0 / 21.2): the rule does not tell
+// them apart.
 // Lists are as long as each other, and so are the workgroups' times: there one kernel does for any length, where the groups are about a multiple of the
 // compute units.  The same for rows that lists name:
 //   bf16, d = 128, 8 heads   256, 2812 62.8 / 56.4;   448, 2812 108.4 / 98.1;   512, 11250 467 / 438;   640, 2812 152.3 / 144.5;   but 288, 2812 76.3 / 83.1;   576, 11250 526 / 540
@@ -794,8 +802,10 @@ static void plan(PagedParams& p, int d, bool mx) {
   p.units = p.Hk * ((G + p.heads_per - 1) / p.heads_per);
   const int least = G <= 2 ? kPgWaves * 4 * 64 * (mx ? 16 : 8) / d : kShWaves * 32;  // what the waves take at a time: 64 to 256
   p.least_shift = __builtin_ctz(least);
-  // Rows of a slice in several rounds (us, rows / heads per group; 512 workgroups / 2048 of 512 rows or more / 2048 of 2048 or more):
-  //   vector ALUs    8 x 65536 rows, 16 heads, d = 128: 577 / 525 / 525;  4 x 16000, 16 heads 74.8 / 69.4 / 74.9;  32 x 4000 8-bit, 8 heads 42.0 / 40.2 / 42.3
+  // Rows of a slice in several rounds (us, rows / heads per group; 512 workgroups / 2048 of 512 rows or more / 2048 of 2048 or more; all sequences as long, down
+  // to half of the longest, down to a tenth):
+  //   vector ALUs    8 x 65536 rows, 16 heads, d = 128: 631 / 633 / 633, 573 / 520 / 519, 444 / 399 / 400;  4 x 16000, 16 heads 84.6 / 85.5 / 84.5, 75.1 / 70.0 / 75.0,
+  //   54.3 / 53.7 / 54.0;  32 x 4000 8-bit, 8 heads 48.3 / 49.3 / 48.7, 42.5 / 40.5 / 42.8, 33.2 / 31.0 / 33.4
   //   matrix pipe, 2048 workgroups of 512 / 1024 / 2048 / 4096 rows or more, sequences down to a tenth of the longest: 32 x 16000 8-bit, 64 heads on 8, d = 128
   //   116.5 / 116.1 / 108.7 / 116.0;  32 x 8000 bf16 103.9 / 101.4 / 107.0 / 100.2;  4 x 30000 bf16, 64 on 4 40.9 / 33.0 / 32.9 / 32.9;  16 x 8000 bf16, d = 64
   //   31.5 / 32.6 / 34.1 / 34.0;  512 workgroups of any size 32 x 16000 8-bit, down to 0.7 of the longest: 179 against 162 / 162 / 165 / 157

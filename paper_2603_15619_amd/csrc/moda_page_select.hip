@@ -339,12 +339,17 @@ __global__ __launch_bounds__(THREADS) void moda_page_choose_kernel(SelectParams 
 static int columns(const SelectParams& p) { return (int)(((long long)p.T + (1 << p.shift) - 1) >> p.shift); }
 
 // How a choice is made: 0: two kernels, else one, a workgroup of so many threads per (sequence, key/value head).  1024 threads, which fill a compute
-// unit / 256, of which several share one / two kernels, us, (sequence, head)s, pages:
-//   d = 128   8, 60 6.2 / 5.7 / 7.8;   8, 180 - / 7.7 / 7.8;   8, 250 8.8 / 8.8 / 7.9;   8, 500 11.1 / 12.9 / 8.8;   8, 2000 25.3 / - / 10.1;   64, 500 11.1 / 12.9 / 9.3
-//             64, 2000 27.6 / - / 19.0;   128, 250 8.9 / 8.9 / 8.9;   128, 500 11.2 / 12.8 / 11.7;   128, 2000 28.7 / - / 27.4;   256, 250 9.3 / 9.2 / 11.4
-//             256, 1000 23.5 / 29.0 / 27.7;   256, 4000 86.6 / - / 104.6
-//             384, 120 12.9 / 8.0 / 12.6;   512, 1000 42.1 / 40.3 / 46.6;   1024, 250 38.1 / 22.6 / 33.2;   1024, 1000 92.9 / 87.2 / 111.6
-//   d = 64    8, 250 7.1 / 6.8 / 8.0;   8, 500 8.8 / 8.9 / 8.3;   128, 500 8.9 / 9.2 / 9.8;   128, 1000 11.3 / 13.3 / 13.2;   256, 1000 15.6 / 18.3 / 17.1;   1024, 1000 50.9 / 40.4 / 53.1
+// unit / 256, of which several share one / two kernels, us, (sequence, head)s, pages of the longest sequence; where it matters all as long, evenly down to half, down to a tenth:
+//   d = 128   8, 60 6.2 / 5.8 / 7.8;   8, 120 7.4 / 6.5 / 7.7;   8, 250 8.9 / 8.9 / 8.0;   8, 500 11.2 / 13.1 / 8.8;   8, 2000 25.4 / - / 10.2;   64, 250 9.0 / 8.9 / 8.2;   64, 2000 28.3 / - / 20.6
+//             128, 250 9.1 / 9.2 / 9.5;   128, 500 12.4 / 15.6 / 12.5, 11.2 / 12.9 / 12.3, 11.3 / 13.1 / 11.8;   128, 2000 29.6 / - / 30.8, 28.6 / - / 24.9, 28.1 / - / 21.2
+//             256, 250 9.9 / 10.5 / 11.7;   256, 1000 25.6 / 29.8 / 30.2, 22.6 / 28.8 / 25.3, 19.9 / 28.2 / 21.2;   256, 4000 96 / - / 117, 81 / - / 98, 58 / - / 79
+//             512, 120 14.4 / 8.9 / 11.8;   512, 1000 47.7 / 43.1 / 52.7, 38.9 / 38.5 / 42.1, 33.9 / 34.5 / 36.1;   512, 2000 99 / - / 116, 81 / - / 98, 59 / - / 70
+//             1024, 250 39.5 / 24.0 / 27.8;   1024, 1000 105.7 / 94.9 / 116.8, 85.9 / 81.2 / 97.7, 63.6 / 58.5 / 65.2
+//   d = 64    8, 250 7.2 / 6.8 / 7.9;   8, 500 8.9 / 8.9 / 8.5;   128, 500 9.7 / 9.5 / 10.0;   128, 1000 12.5 / 16.4 / 13.5, 11.5 / 13.4 / 13.2, 11.3 / 13.1 / 12.3
+//             256, 1000 16.3 / 18.7 / 19.1, 15.6 / 18.1 / 17.0, 12.9 / 16.5 / 16.5;   1024, 1000 55.8 / 45.1 / 52.4, 47.7 / 38.0 / 43.8, 42.3 / 31.8 / 36.4
+// Two kernels would be ahead by a tenth to a quarter where the rule does not take them: 65 to 128 of many pages unless all are as long (above; 72, 2000 28.1 / - / 20.9,
+// 27.9 / - / 19.6, 27.9 / - / 18.2), and little more than 256, a second round for a few (264, 500 25.0 / 20.2 / 19.0, 22.1 / 19.9 / 17.0, 19.8 / 19.2 / 16.7;
+// 264, 2000 67.6 / - / 55.4).
 static int threads_of_one(const SelectParams& p, int d) {
   const int cols = columns(p);
   const long long groups = (long long)p.B * p.Hk;
