@@ -659,7 +659,8 @@ def moda_attn_decode_paged(Q, Kpages, Vpages, page_table, Kdepth=None, Vdepth=No
     """O [B,Hq,d], LSE [B,Hq] for one new token per sequence, under one softmax over the rows of its pages (moda_page_append has
     the cache's arguments; the token's own row is among them) and its depth slots Kdepth/Vdepth [B,Hk,depth_alloc,d] or None.
     lengths [B] (int32): the rows of each sequence; T bounds them (default: all rows that the table has) and is their number where lengths is
-    None.  T also decides the kernels: under a table much wider than the sequences, a T of the longest length that may come is faster.  selected [B,Hk,n] (int32): only the rows of these pages, indices into the sequence's row of page_table, each once, -1: none."""
+    None.  T also decides the kernels: under a table much wider than the sequences, a T of the longest length that may come is faster.
+    selected [B,Hk,n] (int32): only the rows of these pages, indices into the sequence's row of page_table, each once, -1: none."""
     r = (_native_module or _native()).paged(Q, Kpages, Vpages, page_table, Kdepth, Vdepth, lengths, selected, Kscales, Vscales, T,
                                             depth_count, scale, out, lse, workspace)
     if r is not None:

@@ -347,10 +347,10 @@ __global__ __launch_bounds__(kPgWaves * 64, 2) void moda_paged_slices_kernel(Pag
 // Weights go into that product as bf16, rounded as in Columns, or (SPLIT) as sums of two bf16 numbers, a product each: groups of 3 and 4 heads, to which
 // moda_attn_decode gives fp32 weights, are off by O's own rounding alone here too, 0.0017 of their size on N(0,1) data instead of 0.0023.  (Rounded once /
 // split, us, sequences down to half of the longest: 64 x 2100 rows of d = 64, 32 heads on 8, 31.5 / 32.0;  32 x 8000 rows of d = 128, 32 on 8, 133.3 / 133.8;
-// 32 x 16000 8-bit rows, 32 on 8, 141.0 / 145.7.  More heads, whose weights moda_attn_decode rounds as well: 64 on 8 107.1 / 110.7, 256 on 8, 32 columns,
-// 167.8 / 176.4; there it is not done.)
+// 32 x 16000 8-bit rows, 32 on 8, 141.0 / 145.7.  More heads, whose weights moda_attn_decode rounds as well: 64 on 8, down to a tenth, 107.1 / 110.7, 256 on 8,
+// 32 columns, 167.8 / 176.4; there it is not done.)
 
-// Weights (0 or more) as sums of two bf16 numbers, off by 2^-15 of themselves: the largest below x, and the rest, rounded.  Both are above 0 where x is
+// Weights (0 or more) as sums of two bf16 numbers, off by 2^-15 of themselves: the largest one below x, and the rest, rounded.  Both are above 0 where x is
 // (2^-102 or more), so that an infinite value stays one and does not become NaN.
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8& high, bf16x8& rest) {
   u32x4 h;
@@ -775,7 +775,7 @@ static long long rows_bound(const PagedParams& p) { return p.selected ? (long lo
 //                    8 heads   8, 828 9.6 / 9.1;   8, 1031 9.6 / 10.5;   256, 2500 30.3 / 25.8, 27.0 / 22.3, 22.5 / 19.3
 // The limits are those of the form that crosses first, one head in bf16 (8-bit rows on the vector ALUs have their own below 256 groups).  From 256 groups on raggedness
 // decides: at the limit such sequences gain a ninth if all are as long and lose an eighth if they go down to a tenth.  Beyond the limits some forms
-// still gain, by up to a quarter (8 heads, 8 bits, 256 x 1562 rows; 192 groups of 8 heads and 1562 rows 33.6 / 25.0, 29.5 / 22.6, 22.0 / 21.2): the rule does not tell
+// still gain, by up to 27 % (8 heads, 8 bits, 256 x 1562 rows; 192 groups of 8 heads and 1562 rows 33.6 / 25.0, 29.5 / 22.6, 22.0 / 21.2): the rule does not tell
 // them apart.
 // Lists are as long as each other, and so are the workgroups' times: there one kernel does for any length, where the groups are about a multiple of the
 // compute units.  The same for rows that lists name:

@@ -347,8 +347,8 @@ static int columns(const SelectParams& p) { return (int)(((long long)p.T + (1 <<
 //             1024, 250 39.5 / 24.0 / 27.8;   1024, 1000 105.7 / 94.9 / 116.8, 85.9 / 81.2 / 97.7, 63.6 / 58.5 / 65.2
 //   d = 64    8, 250 7.2 / 6.8 / 7.9;   8, 500 8.9 / 8.9 / 8.5;   128, 500 9.7 / 9.5 / 10.0;   128, 1000 12.5 / 16.4 / 13.5, 11.5 / 13.4 / 13.2, 11.3 / 13.1 / 12.3
 //             256, 1000 16.3 / 18.7 / 19.1, 15.6 / 18.1 / 17.0, 12.9 / 16.5 / 16.5;   1024, 1000 55.8 / 45.1 / 52.4, 47.7 / 38.0 / 43.8, 42.3 / 31.8 / 36.4
-// Two kernels would be ahead by a tenth to a quarter where the rule does not take them: 65 to 128 of many pages unless all are as long (above; 72, 2000 28.1 / - / 20.9,
-// 27.9 / - / 19.6, 27.9 / - / 18.2), and little more than 256, a second round for a few (264, 500 25.0 / 20.2 / 19.0, 22.1 / 19.9 / 17.0, 19.8 / 19.2 / 16.7;
+// Two kernels would be ahead by a tenth to a quarter where the rule does not take them: 65 to 128 of many pages (72, 2000 28.1 / - / 20.9, 27.9 / - / 19.6, 27.9 / - / 18.2;
+// 128 unless all are as long, above), and little more than 256, a second round for a few (264, 500 25.0 / 20.2 / 19.0, 22.1 / 19.9 / 17.0, 19.8 / 19.2 / 16.7;
 // 264, 2000 67.6 / - / 55.4).
 static int threads_of_one(const SelectParams& p, int d) {
   const int cols = columns(p);

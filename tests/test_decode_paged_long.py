@@ -2,7 +2,7 @@
 
 The bound on single elements (tests/test_decode_paged.py) is one of sum(w |v|), which long sequences of N(0,1) rows do not make smaller while their
 outputs shrink with the root of their length.  So the outputs of a (sequence, key/value head) are compared as a vector too, ||O - ref|| / ||ref||.
-O's own rounding to bf16 is off by 2^-8 of a value at most and, evenly spread over a step, by 2^-8 / sqrt(3) in the root mean square.  Groups of three
+O's own rounding to bf16 is off by 2^-8 of a value at most and, evenly spread over a step, by 2^-8 / sqrt(3) in the root mean square.  Groups of five
 heads and more round every softmax weight to bf16 too: sum(w e v) with e as spread as that is to sum(w v), v random, as e is to 1.  Together
 sqrt(1/3 + 1/3) 2^-8, and half as much again, more than four deviations of the norm of 64 numbers: 0.0048; without rounded weights 2^-8 itself.  32-bit
 sums add 2^-24 times the logits' size and the like: nothing beside it.  A page of 256 rows that is lost among n changes O by sqrt(256 / n) of it: 0.08 of 40000 rows.
@@ -21,7 +21,7 @@ U = 2.0 ** -8
 
 
 def norm_bound(G):
-    return U if G <= 2 else 1.5 * (2 / 3) ** 0.5 * U
+    return U if G <= 4 else 1.5 * (2 / 3) ** 0.5 * U
 
 
 def off(O, ref, Hk):
@@ -33,12 +33,11 @@ def off(O, ref, Hk):
 
 def compare(O, LSE, r, G, Hk, d):
     to, tl = tolerances(r, d)
-    e = off(f(O), r["O"], Hk)
-    print("   norm %.3f, O %.3f, LSE %.3f of the bounds" % (e.max() / norm_bound(G), (np.abs(f(O) - r["O"]) / to).max(),
-                                                         np.nanmax(np.abs(f(LSE) - r["LSE"]) / tl)), flush=True)
     finite = np.isfinite(r["LSE"])
     assert np.array_equal(finite, np.isfinite(f(LSE)))
-    assert np.all(e <= norm_bound(G)) and np.all(np.abs(f(O) - r["O"]) <= to) and np.all(np.abs(f(LSE)[finite] - r["LSE"][finite]) <= tl[finite])
+    e, eo, el = off(f(O), r["O"], Hk), np.abs(f(O) - r["O"]) / to, np.abs(f(LSE)[finite] - r["LSE"][finite]) / tl[finite]
+    print("   norm %.3f, O %.3f, LSE %.3f of the bounds" % (e.max() / norm_bound(G), eo.max(), el.max(initial=0)), flush=True)
+    assert np.all(e <= norm_bound(G)) and np.all(eo <= 1) and np.all(el <= 1)
 
 
 def workspace_bytes(c, B, Hq, Hk, d, T):
@@ -195,7 +194,7 @@ def test_captured_step_of_many_sequences(G):
     r = P.decode(f(Q), np.nan_to_num(c.K), np.nan_to_num(c.V), c.table, lengths=lengths.tolist())
     to, tl = tolerances(r, 64)
     finite = np.isfinite(r["LSE"])
-    assert np.all(np.abs(f(O) - r["O"]) <= to) and np.all(np.abs(f(LSE) - r["LSE"])[finite] <= tl[finite]) and np.isneginf(f(LSE)[~finite]).all()
+    assert np.all(np.abs(f(O) - r["O"]) <= to) and np.all(np.abs(f(LSE)[finite] - r["LSE"][finite]) <= tl[finite]) and np.isneginf(f(LSE)[~finite]).all()
 
 
 @pytest.mark.gpu
